@@ -182,6 +182,93 @@ int fade_coder_decode_tables(fade_ctx *ctx, const uint16_t *freq_dev, size_t n_s
 int fade_coder_encode_tables_noalloc(fade_ctx *ctx, const uint16_t *freq_dev, const uint8_t *sym_dev, size_t n_steps,
                                      size_t n_streams, uint8_t *out_dev, size_t cap, uint32_t *len_dev);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators around a program's own model: what stands at the ends of its matrix products, for programs that bring their own
+ * model to the quantiser and the coder above. A context without weights serves. All calls enqueue on the context's stream and return without
+ * synchronising, allocate nothing and may be captured into a graph; the results are the same bits from call to call (no
+ * atomics on floats), as a decoder that repeats an encoder's training needs. The current device of the calling thread is left as it was.
+ *   - Matrices are row-major with `*_ld` elements from row to row (at least the width). Elements are FADE_F32 or FADE_BF16 by the
+ *     `*_type` argument, on addresses that are multiples of the element's size; sums and statistics are fp32. Outputs may not overlap inputs
+ *     or one another except where a call says so. Elements between the width and the ld are neither read nor written.
+ *   - Row counts are below 2^31. With no rows only parameter gradients are written (zeros, or left alone when accumulating),
+ *     and pointers to rows may be NULL.
+ *   - `work_dev`: scratch of at least the bytes that the call's *_work function gives, aligned to 16 bytes, contents undefined. Calls that can
+ *     run at the same time (two contexts, two captured graphs) need one each.
+ *   - Wrong sizes, types or alignments and a workspace that is too small: FADE_E_INVALID_ARG, before anything is enqueued.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* Embedding: out[i][:] = scale * table[tokens[i]][:], i < n. tokens_dev [n] of `token_type`; table_dev [vocab][width]; out_dev [n][width].
+ * A token outside [0, vocab) (padding) gives a row of zeros. vocab and width are at most 2^20. */
+enum { FADE_TOKEN_U8 = 0, FADE_TOKEN_I32 = 1, FADE_TOKEN_I64 = 2 };
+int fade_embed(fade_ctx *ctx, const void *tokens_dev, int token_type, size_t n, const void *table_dev, int table_type, size_t table_ld,
+               size_t vocab, size_t width, float scale, void *out_dev, int out_type, size_t out_ld);
+
+/* Its gradient: grad[v][:] = scale * sum of dout[i][:] over the i with tokens[i] == v, in a fixed order of sums; rows of tokens that do not
+ * occur become zero. accumulate != 0: added to grad instead, other rows untouched. grad_dev [vocab][width] fp32.
+ * fade_embed_grad_work is 0 for sizes the call refuses. */
+size_t fade_embed_grad_work(size_t n, size_t vocab, size_t width);
+int fade_embed_grad(fade_ctx *ctx, const void *tokens_dev, int token_type, size_t n, const void *dout_dev, int dout_type, size_t dout_ld,
+                    float scale, float *grad_dev, size_t grad_ld, size_t vocab, size_t width, int accumulate, void *work_dev,
+                    size_t work_bytes);
+
+/* Activation checkpoint of x [rows][width]: 8 bits an element, kept between the passes instead of x. In groups of 32 columns (the last one filled up
+ * with zeros): e the least exponent >= -126 with max|x| <= 127 * 2^e, q = x * 2^-e rounded to the nearest integer, ties to even.
+ * Layout: q as signed bytes [rows][32 G], then e + 127 as bytes [rows][G], G = ceil(width / 32), on an address that is a multiple of 16. A group that holds an infinity or
+ * NaN has the exponent byte 255 and reads back as NaN. q * 2^e is exact in bf16. width is at most 2^20.
+ *   fade_checkpoint_nbytes: 33 G rows (0 for sizes the calls refuse).
+ *   fade_checkpoint: writes keep_dev from x_dev. fade_checkpoint_read: the values it stands for into out_dev.
+ *   fade_checkpoint_weight_grad: the gradient of W in y = x W from x's checkpoint: grad[k][j] = sum over rows of x[row][k] * dy[row][j] (accumulate != 0:
+ *     added to grad); keep_dev of [rows][in_width], dy_dev [rows][out_width], grad_dev [in_width][out_width] fp32. Products are exact (an
+ *     fp32 dy is taken as three bf16 terms that together are dy), sums fp32. Widths are at most 65536. */
+size_t fade_checkpoint_nbytes(size_t rows, size_t width);
+int fade_checkpoint(fade_ctx *ctx, const void *x_dev, int x_type, size_t x_ld, size_t rows, size_t width, void *keep_dev);
+int fade_checkpoint_read(fade_ctx *ctx, const void *keep_dev, size_t rows, size_t width, void *out_dev, int out_type, size_t out_ld);
+size_t fade_checkpoint_weight_grad_work(size_t rows, size_t in_width, size_t out_width);
+int fade_checkpoint_weight_grad(fade_ctx *ctx, const void *keep_dev, size_t rows, size_t in_width, const void *dy_dev, int dy_type, size_t dy_ld,
+                                size_t out_width, float *grad_dev, size_t grad_ld, int accumulate, void *work_dev, size_t work_bytes);
+
+/* The join of a block with the residual stream, and the norm in front of the next block (the operations of Eq. 8 and of the LNs around
+ * Eq. 9-10, for any program's block), per row of `width` columns:
+ *     z = N_u(u),   h = lam * r + sigma(g) * z,   n = N_n(h)
+ * N_u, N_n: FADE_NORM_NONE (the identity), FADE_NORM_LAYER ((x - mean) / sqrt(var + eps) * gamma + beta, biased variance) or FADE_NORM_RMS
+ * (x / sqrt(mean(x^2) + eps) * gamma + beta). n is formed from h before h is rounded. `width` is at most 16384.
+ * The backward pass takes r, u and g again, as they were or as checkpoints of them, forms the statistics anew, and gives, for the gradients
+ * dh (through later uses of h) and dn, those of r, u, g and of the parameters. */
+enum { FADE_NORM_NONE = 0, FADE_NORM_LAYER = 1, FADE_NORM_RMS = 2 };
+typedef struct {
+  uint32_t struct_size;           /* sizeof(fade_join_args) */
+  uint32_t norm_u, norm_n;        /* FADE_NORM_* */
+  float eps;                      /* 0 => 1e-5 */
+  size_t rows, width;
+  uint32_t stream_type;           /* elements of r, h, dh, dr */
+  uint32_t branch_type;           /* elements of u, g, n, dn, du, dg: FADE_BF16, or FADE_F32 with an fp32 stream */
+  uint32_t lam_count;             /* 0: lam is 1; 1: one value; width: one per column (width 1: one value) */
+  uint32_t accumulate;            /* backward: parameter gradients are added to what is there */
+  const float *lam;               /* [lam_count] */
+  const float *gamma_u, *beta_u;  /* [width]; NULL: ones, zeros. Both NULL where the norm is FADE_NORM_NONE */
+  const float *gamma_n, *beta_n;
+  const void *r, *u, *g;          /* [rows][width]; g NULL: no gate (sigma(g) is 1) */
+  size_t r_ld, u_ld, g_ld;
+  /* forward */
+  void *h, *n;                    /* [rows][width]; n NULL: not wanted. h may be r itself (same address, same ld) */
+  size_t h_ld, n_ld;
+  void *keep_r, *keep_u, *keep_g; /* forward: optional checkpoints (fade_checkpoint's layout) of the operands, written as these are read;
+                                     backward: non-NULL keep_u: r, u and g are read from keep_r, keep_u and (gated) keep_g instead */
+  void *keep_n;                   /* forward: optional checkpoint of n as rounded (n itself may then be NULL) */
+  /* backward */
+  const void *dh, *dn;            /* NULL: zeros; not both */
+  size_t dh_ld, dn_ld;
+  void *dr, *du, *dg;             /* any of them NULL: not wanted. dr may be dh itself, du dn itself (same address, same ld) */
+  size_t dr_ld, du_ld, dg_ld;
+  float *d_lam;                   /* [lam_count] */
+  float *d_gamma_u, *d_beta_u, *d_gamma_n, *d_beta_n; /* [width]; NULL: not wanted */
+  void *work;
+  size_t work_bytes;
+} fade_join_args;
+size_t fade_join_grad_work(size_t rows, size_t width);
+int fade_join(fade_ctx *ctx, const fade_join_args *args);
+int fade_join_grad(fade_ctx *ctx, const fade_join_args *args);
+
 /* Debug/test taps: copy an intermediate activation of the most recent step to host as fp32, [B][width].
  * `which` uses FADE_TAP_*; returns the width (0 if unknown); out_host may be NULL to query the width. */
 enum {

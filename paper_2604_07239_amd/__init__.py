@@ -4,8 +4,8 @@ Every function here only marshals arguments; all arithmetic of the path runs in 
 C ABI declared in include/fade.h. There is no CPU fallback: without the built library or without a GPU the
 calls raise.
 """
-from .binding import (BF16, F32, FROZEN, ONLINE_ADAM, TAPS, Config, Fade, FadeError, lib, make_config,  # noqa: F401
-                      weights_nbytes)
+from .binding import (BF16, F32, FROZEN, NORMS, ONLINE_ADAM, TAPS, TOKEN_I32, TOKEN_I64, TOKEN_U8, Config, Fade,  # noqa: F401
+                      FadeError, JoinArgs, lib, make_config, weights_nbytes)
 from .buildlib import LIB, build  # noqa: F401
 
 ONLINE_SUPPORTED = True

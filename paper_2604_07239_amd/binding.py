@@ -8,6 +8,8 @@ import numpy as np
 from .buildlib import LIB
 
 F32, BF16 = 0, 1
+TOKEN_U8, TOKEN_I32, TOKEN_I64 = 0, 1, 2
+NORMS = {"none": 0, "layer": 1, "rms": 2}
 FROZEN, ONLINE_ADAM = 0, 1
 ABI_VERSION = 2
 TAPS = ["X", "CACHE", "H_GLOBAL", "H_LOCAL", "ALPHA", "H_MIX", "Y_DOWN", "Z_BMM", "H_A", "H_COARSE", "H_EXPAND",
@@ -22,6 +24,22 @@ class Config(C.Structure):
                 ("dtype", C.c_uint32), ("update_mode", C.c_uint32),
                 ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("device", C.c_int32), ("hip_stream", C.c_void_p)]
+
+
+class JoinArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("norm_u", C.c_uint32), ("norm_n", C.c_uint32), ("eps", C.c_float),
+                ("rows", C.c_size_t), ("width", C.c_size_t),
+                ("stream_type", C.c_uint32), ("branch_type", C.c_uint32), ("lam_count", C.c_uint32), ("accumulate", C.c_uint32),
+                ("lam", C.c_void_p), ("gamma_u", C.c_void_p), ("beta_u", C.c_void_p), ("gamma_n", C.c_void_p), ("beta_n", C.c_void_p),
+                ("r", C.c_void_p), ("u", C.c_void_p), ("g", C.c_void_p),
+                ("r_ld", C.c_size_t), ("u_ld", C.c_size_t), ("g_ld", C.c_size_t),
+                ("h", C.c_void_p), ("n", C.c_void_p), ("h_ld", C.c_size_t), ("n_ld", C.c_size_t),
+                ("keep_r", C.c_void_p), ("keep_u", C.c_void_p), ("keep_g", C.c_void_p), ("keep_n", C.c_void_p),
+                ("dh", C.c_void_p), ("dn", C.c_void_p), ("dh_ld", C.c_size_t), ("dn_ld", C.c_size_t),
+                ("dr", C.c_void_p), ("du", C.c_void_p), ("dg", C.c_void_p),
+                ("dr_ld", C.c_size_t), ("du_ld", C.c_size_t), ("dg_ld", C.c_size_t),
+                ("d_lam", C.c_void_p), ("d_gamma_u", C.c_void_p), ("d_beta_u", C.c_void_p), ("d_gamma_n", C.c_void_p), ("d_beta_n", C.c_void_p),
+                ("work", C.c_void_p), ("work_bytes", C.c_size_t)]
 
 
 def make_config(B, T, D, H, d_low=0, cache_chunk=0, conv_k=0, dtype=BF16, update_mode=FROZEN, lr=0.0, beta1=0.0,
@@ -67,6 +85,22 @@ def lib():
         L.fade_coder_encode_tables.argtypes = [vp, vp, vp, sz, sz, vp, sz, vp]
         L.fade_coder_decode_tables.argtypes = [vp, vp, sz, sz, vp, sz, vp, vp]
         L.fade_coder_encode_tables_noalloc.argtypes = [vp, vp, vp, sz, sz, vp, sz, vp]
+        i, f = C.c_int, C.c_float
+        L.fade_embed.argtypes = [vp, vp, i, sz, vp, i, sz, sz, sz, f, vp, i, sz]
+        L.fade_embed_grad_work.restype = sz
+        L.fade_embed_grad_work.argtypes = [sz, sz, sz]
+        L.fade_embed_grad.argtypes = [vp, vp, i, sz, vp, i, sz, f, vp, sz, sz, sz, i, vp, sz]
+        L.fade_checkpoint_nbytes.restype = sz
+        L.fade_checkpoint_nbytes.argtypes = [sz, sz]
+        L.fade_checkpoint.argtypes = [vp, vp, i, sz, sz, sz, vp]
+        L.fade_checkpoint_read.argtypes = [vp, vp, sz, sz, vp, i, sz]
+        L.fade_checkpoint_weight_grad_work.restype = sz
+        L.fade_checkpoint_weight_grad_work.argtypes = [sz, sz, sz]
+        L.fade_checkpoint_weight_grad.argtypes = [vp, vp, sz, sz, vp, i, sz, sz, vp, sz, i, vp, sz]
+        L.fade_join_grad_work.restype = sz
+        L.fade_join_grad_work.argtypes = [sz, sz]
+        L.fade_join.argtypes = [vp, C.POINTER(JoinArgs)]
+        L.fade_join_grad.argtypes = [vp, C.POINTER(JoinArgs)]
         L.fade_tap.restype = sz
         L.fade_tap.argtypes = [vp, C.c_int, vp, sz]
         L.fade_get_weights.argtypes = [vp, vp, sz]
@@ -96,6 +130,10 @@ def _hp(a):
 
 def _dp(t):
     return None if t is None else C.c_void_p(t.data_ptr())
+
+
+_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16}
+_TOKENS = {"torch.uint8": TOKEN_U8, "torch.int32": TOKEN_I32, "torch.int64": TOKEN_I64}
 
 
 class Fade:
@@ -217,6 +255,152 @@ class Fade:
 
     def coder_decode_tables(self, freq_dev, n_steps, n_streams, in_dev, cap, len_dev, sym_dev):
         self._chk(self.L.fade_coder_decode_tables(self.h, _dp(freq_dev), n_steps, n_streams, _dp(in_dev), cap, _dp(len_dev), _dp(sym_dev)))
+
+    # -- operators around a program's own model -----------------------------------------------------
+    # Tensors are checked here for what the C ABI cannot see: their device, type, shape and strides. Everything is enqueued on
+    # the context's stream; nothing is allocated.
+    def _bad(self, what):
+        raise FadeError(-1, what)
+
+    def _rows(self, t, name, rows=None, width=None, f32=False):
+        """(pointer, type, ld) of a matrix [rows][width] whose columns are neighbours."""
+        kind = _TYPES.get(str(t.dtype))
+        if kind is None or (f32 and kind != F32) or t.dim() != 2 or not t.is_cuda or t.device.index != self.cfg.device:
+            self._bad(f"{name}: a matrix of {'float32' if f32 else 'float32 or bfloat16'} on the context's device is needed")
+        if (rows is not None and t.shape[0] != rows) or (width is not None and t.shape[1] != width):
+            self._bad(f"{name}: shape {tuple(t.shape)} where [{rows}, {width}] is needed")
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            self._bad(f"{name}: neighbouring columns have to be neighbours in memory")
+        return t.data_ptr(), kind, (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+    def _vector(self, t, name, count):
+        if t is None:
+            return None
+        if str(t.dtype) != "torch.float32" or not t.is_cuda or t.device.index != self.cfg.device or t.numel() != count or not t.is_contiguous():
+            self._bad(f"{name}: {count} contiguous float32 values on the context's device are needed")
+        return t.data_ptr()
+
+    def _bytes(self, t, name, least):
+        """Pointer to a buffer of at least `least` bytes."""
+        if not t.is_cuda or t.device.index != self.cfg.device or not t.is_contiguous() or t.numel() * t.element_size() < least:
+            self._bad(f"{name}: a contiguous buffer of {least} bytes on the context's device is needed")
+        return t.data_ptr()
+
+    def _tokens(self, t):
+        kind = _TOKENS.get(str(t.dtype))
+        if kind is None or not t.is_cuda or t.device.index != self.cfg.device or not t.is_contiguous():
+            self._bad("tokens: contiguous uint8, int32 or int64 values on the context's device are needed")
+        return t.data_ptr(), kind, t.numel()
+
+    def embed(self, tokens, table, out, scale=1.0):
+        """out[i] = scale * table[tokens[i]]; tokens outside the table give zeros."""
+        tp, tk, n = self._tokens(tokens)
+        ep, ek, eld = self._rows(table, "table")
+        op, ok, old = self._rows(out, "out", n, table.shape[1])
+        self._chk(self.L.fade_embed(self.h, tp, tk, n, ep, ek, eld, table.shape[0], table.shape[1], scale, op, ok, old))
+
+    def embed_grad_work(self, n, vocab, width):
+        return self.L.fade_embed_grad_work(n, vocab, width)
+
+    def embed_grad(self, tokens, dout, grad, work, scale=1.0, accumulate=False):
+        """grad[v] = scale * sum of dout[i] where tokens[i] == v, or that added to grad."""
+        tp, tk, n = self._tokens(tokens)
+        gp, _, gld = self._rows(grad, "grad", f32=True)
+        vocab, width = grad.shape
+        dp, dk, dld = self._rows(dout, "dout", n, width)
+        wp, wn = self._bytes(work, "work", 0), work.numel() * work.element_size()
+        self._chk(self.L.fade_embed_grad(self.h, tp, tk, n, dp, dk, dld, scale, gp, gld, vocab, width, int(accumulate), wp, wn))
+
+    def checkpoint_nbytes(self, rows, width):
+        return self.L.fade_checkpoint_nbytes(rows, width)
+
+    def checkpoint(self, x, keep):
+        """Writes the 8-bit checkpoint of x [rows][width] into keep (checkpoint_nbytes(rows, width) bytes)."""
+        xp, xk, xld = self._rows(x, "x")
+        rows, width = x.shape
+        self._chk(self.L.fade_checkpoint(self.h, xp, xk, xld, rows, width, self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, width))))
+
+    def checkpoint_read(self, keep, out):
+        """The values a checkpoint stands for into out [rows][width]."""
+        op, ok, old = self._rows(out, "out")
+        rows, width = out.shape
+        self._chk(self.L.fade_checkpoint_read(self.h, self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, width)), rows, width, op, ok, old))
+
+    def checkpoint_weight_grad_work(self, rows, in_width, out_width):
+        return self.L.fade_checkpoint_weight_grad_work(rows, in_width, out_width)
+
+    def checkpoint_weight_grad(self, keep, dy, grad, work, accumulate=False):
+        """grad [in][out] = x^T dy from the checkpoint of x [rows][in] and dy [rows][out], or that added to grad."""
+        dp, dk, dld = self._rows(dy, "dy")
+        rows, n = dy.shape
+        gp, _, gld = self._rows(grad, "grad", None, n, f32=True)
+        k = grad.shape[0]
+        kp, wp = self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, k)), self._bytes(work, "work", 0)
+        self._chk(self.L.fade_checkpoint_weight_grad(self.h, kp, rows, k, dp, dk, dld, n, gp, gld, int(accumulate), wp, work.numel() * work.element_size()))
+
+    def _join_args(self, rows, width, stream, branch, norm_u, norm_n, eps, lam, params, matrices, keeps):
+        """matrices: (name, tensor, whether it is one of the stream's); stream, branch: element types, None where nothing says"""
+        if norm_u not in NORMS or norm_n not in NORMS:
+            self._bad(f"norm: one of {', '.join(NORMS)} is needed")
+        a = JoinArgs(struct_size=C.sizeof(JoinArgs), norm_u=NORMS[norm_u], norm_n=NORMS[norm_n], eps=eps, rows=rows, width=width)
+        kinds = [stream, branch]
+        for name, t, of_stream in matrices:
+            if t is None:
+                continue
+            p, kind, ld = self._rows(t, name, rows, width)
+            side = 0 if of_stream else 1
+            if kinds[side] is None:
+                kinds[side] = kind
+            elif kinds[side] != kind:
+                self._bad(f"{name}: another type than the {'stream' if of_stream else 'branch'}'s other matrices")
+            setattr(a, name, p)
+            setattr(a, name + "_ld", ld)
+        # an operand that nobody gives has any type that goes with the other's
+        a.stream_type = kinds[0] if kinds[0] is not None else (kinds[1] or F32)
+        a.branch_type = kinds[1] if kinds[1] is not None else a.stream_type
+        if lam is not None:
+            a.lam_count = lam.numel()
+            if a.lam_count not in (1, width):
+                self._bad(f"lam: 1 or {width} values are needed")
+            a.lam = self._vector(lam, "lam", a.lam_count)
+        for name, t in params:
+            if t is not None:
+                setattr(a, name, self._vector(t, name, a.lam_count if name == "d_lam" else width))
+        for name, t in keeps:
+            if t is not None:
+                setattr(a, name, self._bytes(t, name, self.L.fade_checkpoint_nbytes(rows, width)))
+        return a
+
+    def join(self, h, n=None, *, r, u, g=None, lam=None, norm_u="layer", norm_n="layer", gamma_u=None, beta_u=None, gamma_n=None, beta_n=None, eps=0.0,
+             keep_r=None, keep_u=None, keep_g=None, keep_n=None):
+        """h = lam * r + sigma(g) * norm_u(u) and n = norm_n(h), and 8-bit checkpoints of r, u, g and n where buffers are given."""
+        rows, width = r.shape
+        a = self._join_args(rows, width, None, None, norm_u, norm_n, eps, lam,
+                            (("gamma_u", gamma_u), ("beta_u", beta_u), ("gamma_n", gamma_n), ("beta_n", beta_n)),
+                            (("r", r, True), ("h", h, True), ("u", u, False), ("g", g, False), ("n", n, False)),
+                            (("keep_r", keep_r), ("keep_u", keep_u), ("keep_g", keep_g), ("keep_n", keep_n)))
+        self._chk(self.L.fade_join(self.h, C.byref(a)))
+
+    def join_grad_work(self, rows, width):
+        return self.L.fade_join_grad_work(rows, width)
+
+    def join_grad(self, dh, dn, work, *, r=None, u=None, g=None, keep_r=None, keep_u=None, keep_g=None, lam=None, norm_u="layer", norm_n="layer", gamma_u=None,
+                  beta_u=None, gamma_n=None, beta_n=None, eps=0.0, dr=None, du=None, dg=None, d_lam=None, d_gamma_u=None, d_beta_u=None, d_gamma_n=None,
+                  d_beta_n=None, accumulate=False):
+        """The gradients of join() for those of h and n (either may be None), from its operands or from their checkpoints."""
+        like = dh if dh is not None else dn
+        if like is None:
+            self._bad("neither dh nor dn")
+        rows, width = like.shape
+        a = self._join_args(rows, width, None, None, norm_u, norm_n, eps, lam,
+                            (("gamma_u", gamma_u), ("beta_u", beta_u), ("gamma_n", gamma_n), ("beta_n", beta_n), ("d_lam", d_lam), ("d_gamma_u", d_gamma_u),
+                             ("d_beta_u", d_beta_u), ("d_gamma_n", d_gamma_n), ("d_beta_n", d_beta_n)),
+                            (("r", r, True), ("dh", dh, True), ("dr", dr, True), ("u", u, False), ("g", g, False), ("dn", dn, False), ("du", du, False),
+                             ("dg", dg, False)),
+                            (("keep_r", keep_r), ("keep_u", keep_u), ("keep_g", keep_g)))
+        a.accumulate = int(accumulate)
+        a.work, a.work_bytes = self._bytes(work, "work", 0), work.numel() * work.element_size()
+        self._chk(self.L.fade_join_grad(self.h, C.byref(a)))
 
     # -- profiling -------------------------------------------------------------------------------
     def profile(self, enable):

@@ -14,6 +14,8 @@
 
 #include "../../include/fade.h"
 #include "fade_kernels.h"
+#include "fade_ops.h"
+#include "fade_op_checks.h"
 #include "fade_lanes.h"
 #include "fade_rules.h"
 
@@ -1436,6 +1438,56 @@ int run_loop(fade_ctx *c, uint8_t *bytes_dev, size_t n, size_t first, size_t cou
 
 }  // namespace
 
+// what the entry points of the operators around a program's own model share
+// The calling thread's device for the length of a call: launches go to the context's, the caller's is back afterwards.
+namespace {
+struct OnDevice {
+  int before = -1;
+  hipError_t err;
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&before);
+    if (err == hipSuccess && before == device) before = -1;
+    else if (err == hipSuccess) err = hipSetDevice(device);
+    else before = -1;
+  }
+  ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+// Nothing throws past an entry point: where there is no memory for the message, the code is all there is.
+int op_refuse(fade_ctx *c, const char *call, const char *why) noexcept {
+  try { c->err = std::string(call) + ": " + why; } catch (...) {}
+  return FADE_E_INVALID_ARG;
+}
+int op_done(fade_ctx *c, hipError_t e, const char *what) noexcept {
+  if (e == hipSuccess) return FADE_OK;
+  try { return hip_fail(c, e, what); } catch (...) { return e == hipErrorOutOfMemory ? FADE_E_OOM : FADE_E_HIP; }
+}
+template <typename F> int op_launch(fade_ctx *c, const char *what, F &&launch) noexcept {
+  OnDevice on(c->cfg.device);
+  if (on.err != hipSuccess) return op_done(c, on.err, "hipSetDevice");
+  return op_done(c, launch(c->stream), what);
+}
+OpKeep op_keep(const void *p, size_t rows, size_t width) { return OpKeep{static_cast<uint8_t *>(const_cast<void *>(p)), rows, (int)((width + 31) / 32)}; }
+JoinArgs op_join(const fade_join_args *a, bool grad) {
+  JoinArgs j{};
+  j.rows = (int)a->rows; j.width = (int)a->width; j.norm_u = (int)a->norm_u; j.norm_n = (int)a->norm_n;
+  j.eps = a->eps == 0.0f ? 1e-5f : a->eps;
+  j.lam_count = (int)a->lam_count; j.accumulate = a->accumulate != 0;
+  j.stream_f32 = a->stream_type == FADE_F32; j.branch_f32 = a->branch_type == FADE_F32; j.kept = grad && a->keep_u;
+  j.lam = a->lam; j.gamma_u = a->gamma_u; j.beta_u = a->beta_u; j.gamma_n = a->gamma_n; j.beta_n = a->beta_n;
+  j.r = a->r; j.u = a->u; j.g = a->g; j.r_ld = a->r_ld; j.u_ld = a->u_ld; j.g_ld = a->g_ld;
+  j.keep_r = static_cast<uint8_t *>(a->keep_r); j.keep_u = static_cast<uint8_t *>(a->keep_u); j.keep_g = static_cast<uint8_t *>(a->keep_g);
+  if (!grad) {
+    j.h = a->h; j.h_ld = a->h_ld; j.n = a->n; j.n_ld = a->n_ld; j.keep_n = static_cast<uint8_t *>(a->keep_n);
+    return j;
+  }
+  j.dh = a->dh; j.dh_ld = a->dh_ld; j.dn = a->dn; j.dn_ld = a->dn_ld;
+  j.dr = a->dr; j.dr_ld = a->dr_ld; j.du = a->du; j.du_ld = a->du_ld; j.dg = a->dg; j.dg_ld = a->dg_ld;
+  j.d_lam = a->d_lam; j.d_gamma_u = a->d_gamma_u; j.d_beta_u = a->d_beta_u; j.d_gamma_n = a->d_gamma_n; j.d_beta_n = a->d_beta_n;
+  j.work = static_cast<float *>(a->work);
+  return j;
+}
+}  // namespace
+
 // ---------------------------------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------------------------------
@@ -1973,6 +2025,86 @@ int fade_coder_decode_tables(fade_ctx *c, const uint16_t *freq_dev, size_t n_ste
                              const uint32_t *len_dev, uint8_t *sym_dev) {
   return coder_tables(c, freq_dev, sym_dev, n_steps, n_streams, const_cast<uint8_t *>(in_dev), cap, const_cast<uint32_t *>(len_dev),
                       CODE_DECODE);
+}
+
+// ---- operators around a program's own model
+int fade_embed(fade_ctx *c, const void *tokens_dev, int token_type, size_t n, const void *table_dev, int table_type, size_t table_ld, size_t vocab, size_t width,
+               float scale, void *out_dev, int out_type, size_t out_ld) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::embed(tokens_dev, token_type, n, table_dev, table_type, table_ld, vocab, width, out_dev, out_type, out_ld))
+    return op_refuse(c, "fade_embed", why);
+  if (n == 0) return FADE_OK;
+  return op_launch(c, "fade_embed", [&](hipStream_t s) {
+    return fade_embed_launch(OpTokens{tokens_dev, token_type}, n, OpMat{table_dev, table_ld, table_type == FADE_F32}, vocab, width, scale,
+                             OpMat{out_dev, out_ld, out_type == FADE_F32}, s);
+  });
+}
+
+size_t fade_embed_grad_work(size_t n, size_t vocab, size_t width) {
+  return fade_op::embed_sizes(n, vocab, width) ? fade_embed_grad_bytes(n, vocab, width) : 0;
+}
+
+int fade_embed_grad(fade_ctx *c, const void *tokens_dev, int token_type, size_t n, const void *dout_dev, int dout_type, size_t dout_ld, float scale,
+                    float *grad_dev, size_t grad_ld, size_t vocab, size_t width, int accumulate, void *work_dev, size_t work_bytes) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::embed_grad(tokens_dev, token_type, n, dout_dev, dout_type, dout_ld, grad_dev, grad_ld, vocab, width, work_dev, work_bytes,
+                                            fade_embed_grad_work(n, vocab, width)))
+    return op_refuse(c, "fade_embed_grad", why);
+  return op_launch(c, "fade_embed_grad", [&](hipStream_t s) {
+    return fade_embed_grad_launch(OpTokens{tokens_dev, token_type}, n, OpMat{dout_dev, dout_ld, dout_type == FADE_F32}, scale, grad_dev, grad_ld, vocab, width,
+                                  accumulate != 0, work_dev, s);
+  });
+}
+
+size_t fade_checkpoint_nbytes(size_t rows, size_t width) { return fade_op::keep_sizes(rows, width) ? 33 * ((width + 31) / 32) * rows : 0; }
+
+int fade_checkpoint(fade_ctx *c, const void *x_dev, int x_type, size_t x_ld, size_t rows, size_t width, void *keep_dev) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::checkpoint(x_dev, x_type, x_ld, rows, width, keep_dev)) return op_refuse(c, "fade_checkpoint", why);
+  if (rows == 0) return FADE_OK;
+  return op_launch(c, "fade_checkpoint", [&](hipStream_t s) {
+    return fade_keep_launch(OpMat{x_dev, x_ld, x_type == FADE_F32}, width, op_keep(keep_dev, rows, width), s);
+  });
+}
+
+int fade_checkpoint_read(fade_ctx *c, const void *keep_dev, size_t rows, size_t width, void *out_dev, int out_type, size_t out_ld) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::checkpoint(out_dev, out_type, out_ld, rows, width, keep_dev)) return op_refuse(c, "fade_checkpoint_read", why);
+  if (rows == 0) return FADE_OK;
+  return op_launch(c, "fade_checkpoint_read", [&](hipStream_t s) {
+    return fade_keep_read_launch(op_keep(keep_dev, rows, width), width, OpMat{out_dev, out_ld, out_type == FADE_F32}, s);
+  });
+}
+
+size_t fade_checkpoint_weight_grad_work(size_t rows, size_t in_width, size_t out_width) {
+  if (!fade_op::grad_sizes(rows, in_width, out_width)) return 0;
+  return std::max<size_t>(16, fade_keep_grad_bytes(rows, in_width, out_width));
+}
+
+int fade_checkpoint_weight_grad(fade_ctx *c, const void *keep_dev, size_t rows, size_t in_width, const void *dy_dev, int dy_type, size_t dy_ld, size_t out_width,
+                                float *grad_dev, size_t grad_ld, int accumulate, void *work_dev, size_t work_bytes) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::weight_grad(keep_dev, rows, in_width, dy_dev, dy_type, dy_ld, out_width, grad_dev, grad_ld, work_dev, work_bytes,
+                                             fade_checkpoint_weight_grad_work(rows, in_width, out_width)))
+    return op_refuse(c, "fade_checkpoint_weight_grad", why);
+  return op_launch(c, "fade_checkpoint_weight_grad", [&](hipStream_t s) {
+    return fade_keep_grad_launch(op_keep(keep_dev, rows, in_width), in_width, OpMat{dy_dev, dy_ld, dy_type == FADE_F32}, out_width, grad_dev, grad_ld,
+                                 accumulate != 0, work_dev, s);
+  });
+}
+
+size_t fade_join_grad_work(size_t rows, size_t width) { return fade_op::join_sizes(rows, width) ? fade_join_grad_bytes(rows, width) : 0; }
+
+int fade_join(fade_ctx *c, const fade_join_args *a) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::join(a)) return op_refuse(c, "fade_join", why);
+  return op_launch(c, "fade_join", [&](hipStream_t s) { return fade_join_launch(op_join(a, false), s); });
+}
+
+int fade_join_grad(fade_ctx *c, const fade_join_args *a) {
+  if (!c) return FADE_E_INVALID_ARG;
+  if (const char *why = fade_op::join_grad(a, a ? fade_join_grad_work(a->rows, a->width) : 0)) return op_refuse(c, "fade_join_grad", why);
+  return op_launch(c, "fade_join_grad", [&](hipStream_t s) { return fade_join_grad_launch(op_join(a, true), s); });
 }
 
 size_t fade_tap(fade_ctx *c, int which, float *out_host, size_t cap_floats) {

@@ -1,0 +1,357 @@
+// fade_embed.hip — embedding lookup with scaling, and its gradient by sorted tokens (gfx950).
+//
+// Forward: y[i] = scale * E[t_i], one pass over the output; bounded by its bytes.
+// Gradient: G[v] = scale * sum of dy[i] over t_i = v. Atomics would add the rows of a token in any order, and the result would
+// differ from run to run; a decoder that repeats an encoder's training would leave it. So the positions are sorted by token first
+// (stable, hence ascending in every token's run), cut into pieces of equal length, and each piece is summed in order; a run that
+// crosses a piece's border leaves partial sums that a second kernel adds in order. The sort moves a few words a token, the sums
+// read dy once: from some hundred columns on the bytes of dy and G bound it.
+#include "../../include/fade.h"
+#include "fade_op_rules.h"
+#include "fade_ops.h"
+
+namespace {
+using namespace fade_op;
+
+constexpr uint32_t NO_TOKEN = 0xffffffffu;
+__device__ __forceinline__ uint32_t token_at(const OpTokens &t, size_t i, uint32_t vocab) {
+  if (t.type == FADE_TOKEN_U8) {
+    const uint32_t v = static_cast<const uint8_t *>(t.p)[i];
+    return v < vocab ? v : NO_TOKEN;
+  }
+  if (t.type == FADE_TOKEN_I32) {
+    const uint32_t v = static_cast<const uint32_t *>(t.p)[i];  // a negative one is past every vocabulary
+    return v < vocab ? v : NO_TOKEN;
+  }
+  const uint64_t v = static_cast<const uint64_t *>(t.p)[i];
+  return v < vocab ? (uint32_t)v : NO_TOKEN;
+}
+
+// 2^shift lanes on a row, 8 columns each
+template <typename TT, typename TO>
+__global__ __launch_bounds__(256) void embed_kernel(OpTokens t, size_t n, const TT *table, size_t table_ld, uint32_t vocab, int width, float scale,
+                                                    TO *out, size_t out_ld, int shift) {
+  const size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
+  if (row >= n) return;
+  const uint32_t v = token_at(t, row, vocab);
+  for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < width; c += 8 << shift) {
+    float x[8];
+    OpRaw<TT> in;
+    if (v != NO_TOKEN) in.load(table + v * table_ld + c, width - c);
+    else in.zero();
+    in.get(x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = v != NO_TOKEN ? x[k] * scale : 0.0f;
+    OpRaw<TO> o;
+    o.put(x);
+    o.store(out + row * out_ld + c, width - c);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// The sort: least significant digit first, one or two passes of up to 10 bits. A workgroup counts the digits of its tile, a wavefront per
+// digit adds the counts of the tiles in front, and the tiles' elements go to their places, in order.
+// ---------------------------------------------------------------------------------------------------
+// counts of the tile's digits; the first pass reads the tokens themselves and clears the flags of the tokens that occur
+template <bool FIRST>
+__global__ __launch_bounds__(256) void sort_count_kernel(OpTokens t, GradPlan p, const uint32_t *keys, const uint32_t *total, uint32_t *hist,
+                                                         uint8_t *flags, int low) {
+  __shared__ uint32_t count[MAX_DIGITS];
+  const uint32_t digits = 1u << p.bits;
+  for (uint32_t d = threadIdx.x; d < digits; d += 256) count[d] = 0;
+  __syncthreads();
+  const uint32_t n = FIRST ? p.n : total[MAX_DIGITS];
+  const size_t begin = (size_t)blockIdx.x * 256 * p.items;
+  for (int i = 0; i < p.items; ++i) {
+    const size_t at = begin + i * 256 + threadIdx.x;
+    if (at >= n) break;
+    const uint32_t k = FIRST ? token_at(t, at, p.vocab) : keys[at];
+    if (k != NO_TOKEN) atomicAdd(&count[(k >> low) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (uint32_t d = threadIdx.x; d < digits; d += 256) hist[(size_t)d * p.tiles + blockIdx.x] = count[d];
+  if (FIRST) {
+    uint4 *f = reinterpret_cast<uint4 *>(flags);
+    const size_t words = ((size_t)p.vocab + 15) / 16;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) f[i] = make_uint4(0, 0, 0, 0);
+  }
+}
+// a wavefront per digit: counts of a tile -> counts of the tiles in front of it, and the digit's total
+__global__ __launch_bounds__(256) void sort_scan_kernel(GradPlan p, uint32_t *hist, uint32_t *total) {
+  const uint32_t d = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (d >= 1u << p.bits) return;
+  uint32_t *h = hist + (size_t)d * p.tiles;
+  uint32_t sum = 0;
+  for (uint32_t i = 0; i < p.tiles; i += 64) {
+    const uint32_t v = i + lane < p.tiles ? h[i + lane] : 0;
+    const uint32_t upto = fade_lanes_scan(v);
+    if (i + lane < p.tiles) h[i + lane] = sum + upto - v;
+    sum += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  if (lane == 0) total[d] = sum;
+}
+// Every element to its place: the digits in front, the same digit in the tiles in front, in the wavefronts in front, and in front
+// in its own wavefront, whose 64 elements at a time compare their digits bit by bit (ballots).
+template <bool FIRST, bool LAST>
+__global__ __launch_bounds__(256) void sort_place_kernel(OpTokens t, GradPlan p, const uint32_t *keys, const uint32_t *pos, const uint32_t *hist,
+                                                         uint32_t *total, uint32_t *keys_out, uint32_t *pos_out, uint8_t *flags, int low) {
+  __shared__ uint32_t count[4][MAX_DIGITS];  // per wavefront, then where its first element of the digit goes
+  __shared__ uint32_t wave_sum[4];
+  const uint32_t digits = 1u << p.bits;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (uint32_t d = tid; d < 4 * MAX_DIGITS; d += 256) count[d / MAX_DIGITS][d % MAX_DIGITS] = 0;
+  __syncthreads();
+  const uint32_t n = FIRST ? p.n : total[MAX_DIGITS];
+  const size_t begin = (size_t)blockIdx.x * 256 * p.items + (size_t)wave * 64 * p.items;
+  uint32_t key[16], rank[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    key[i] = NO_TOKEN;
+    if (i < p.items) {
+      const size_t at = begin + i * 64 + lane;
+      if (at < n) key[i] = FIRST ? token_at(t, at, p.vocab) : keys[at];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    rank[i] = 0;
+    if (i < p.items) {
+      const bool in = key[i] != NO_TOKEN;
+      const uint32_t d = (key[i] >> low) & (digits - 1);
+      uint64_t same = __ballot(in);
+      for (int b = 0; b < p.bits; ++b) {
+        const bool one = (d >> b) & 1;
+        const uint64_t m = __ballot(one);
+        same &= one ? m : ~m;
+      }
+      const uint64_t below = same & (((uint64_t)1 << lane) - 1);
+      if (in) rank[i] = count[wave][d] + (uint32_t)__popcll(below);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (in && below == 0) count[wave][d] += (uint32_t)__popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+  __syncthreads();
+  // digits in front: an exclusive scan of the totals, four digits per thread
+  uint32_t v[4], sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t d = tid * 4 + j;
+    v[j] = sum;
+    sum += d < digits ? total[d] : 0;
+  }
+  const uint32_t upto = fade_lanes_scan(sum);
+  if (lane == 63) wave_sum[wave] = upto;
+  __syncthreads();
+  uint32_t before = upto - sum;
+  for (int w = 0; w < wave; ++w) before += wave_sum[w];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t d = tid * 4 + j;
+    if (d >= digits) break;
+    uint32_t to = before + v[j] + hist[(size_t)d * p.tiles + blockIdx.x];
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t c = count[w][d];
+      count[w][d] = to;
+      to += c;
+    }
+  }
+  if (FIRST && blockIdx.x == 0 && tid == 255) total[MAX_DIGITS] = before + sum;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < p.items && key[i] != NO_TOKEN) {
+      const size_t at = begin + i * 64 + lane;
+      const uint32_t to = count[wave][(key[i] >> low) & (digits - 1)] + rank[i];
+      keys_out[to] = key[i];
+      pos_out[to] = FIRST ? (uint32_t)at : pos[at];
+      if (LAST) flags[key[i]] = 1;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// The sums
+// ---------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void grad_clear_kernel(GradPlan p, const uint8_t *flags, float *grad, size_t grad_ld, int width) {
+  const size_t v = (size_t)blockIdx.x * (256 >> p.shift) + (threadIdx.x >> p.shift);
+  if (v >= p.vocab || flags[v]) return;
+  OpRaw<float> o;
+  o.zero();
+  for (int c = (threadIdx.x & ((1 << p.shift) - 1)) * 8; c < width; c += 8 << p.shift) o.store(grad + v * grad_ld + c, width - c);
+}
+struct SumArgs {
+  const uint32_t *keys, *pos, *total;
+  const void *dout;
+  size_t dout_ld;
+  float scale;
+  float *grad;
+  size_t grad_ld;
+  float *part;   // [pieces][2][part_ld]: a run that came from the piece in front; one that starts here and goes on
+  int width, part_ld;
+  bool accumulate;
+};
+__device__ __forceinline__ void grad_put(const SumArgs &a, uint32_t v, int c, float x[8]) {
+  float *dst = a.grad + v * a.grad_ld + c;
+  OpRaw<float> o;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] *= a.scale;
+  if (a.accumulate) {
+    float old[8];
+    o.load(dst, a.width - c);
+    o.get(old);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] += old[k];
+  }
+  o.put(x);
+  o.store(dst, a.width - c);
+}
+template <typename T> __global__ __launch_bounds__(256) void grad_sum_kernel(GradPlan p, SumArgs a) {
+  const uint32_t g = blockIdx.x * (256 >> p.shift) + (threadIdx.x >> p.shift);
+  const uint32_t piece = g / p.strips;
+  const int c = ((g - piece * p.strips) << (p.shift + 3)) + (threadIdx.x & ((1 << p.shift) - 1)) * 8;
+  const uint32_t n = a.total[MAX_DIGITS];
+  const size_t first = (size_t)piece * p.piece;
+  if (first >= n || c >= a.width) return;
+  const uint32_t begin = (uint32_t)first, end = n - begin < p.piece ? n : begin + p.piece;
+  uint32_t cur = a.keys[begin];
+  bool came = begin > 0 && a.keys[begin - 1] == cur;
+  float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  auto leave = [&](bool goes) {  // the run that ends here, or at the piece's end
+    if (came || goes) {
+      OpRaw<float> o;
+      o.put(acc);
+      o.store(a.part + ((size_t)piece * 2 + (came ? 0 : 1)) * a.part_ld + c, 8);
+    } else {
+      grad_put(a, cur, c, acc);
+    }
+  };
+  const T *src = static_cast<const T *>(a.dout) + c;
+  for (uint32_t i = begin; i < end; i += 4) {
+    uint32_t key[4];
+    OpRaw<T> row[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t at = i + j < end ? i + j : end - 1;
+      key[j] = a.keys[at];
+      row[j].load(src + a.pos[at] * a.dout_ld, a.width - c);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i + j >= end) break;
+      if (key[j] != cur) {
+        leave(false);
+        cur = key[j];
+        came = false;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
+      }
+      float x[8];
+      row[j].get(x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] += x[k];
+    }
+  }
+  leave(end < n && a.keys[end] == cur);
+}
+// The runs that cross pieces: the workgroup of the piece a run starts in adds its partial sums, its groups of lanes in equal ranges of the pieces
+// in between, then the groups' sums in order.
+__global__ __launch_bounds__(256) void grad_join_kernel(GradPlan p, SumArgs a) {
+  __shared__ float sums[256][8];
+  const uint32_t piece = blockIdx.x / p.strips;
+  const int strip = (int)(blockIdx.x - piece * p.strips), group = threadIdx.x >> p.shift, groups = 256 >> p.shift;
+  const int lane = threadIdx.x & ((1 << p.shift) - 1), c = (strip << (p.shift + 3)) + lane * 8;
+  const uint32_t n = a.total[MAX_DIGITS];
+  const size_t first = (size_t)piece * p.piece, next = first + p.piece;
+  if (next >= n) return;
+  const uint32_t v = a.keys[next - 1];
+  if (a.keys[next] != v || (a.keys[first] == v && first > 0 && a.keys[first - 1] == v)) return;
+  uint32_t lo = (uint32_t)next, hi = n - 1;  // the last position of the run
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo + 1) / 2;
+    if (a.keys[mid] == v) lo = mid;
+    else hi = mid - 1;
+  }
+  const uint32_t last = lo / p.piece, count = last - piece, per = (count + groups - 1) / groups;
+  float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  const uint32_t from = piece + 1 + group * per, to = from + per < last + 1 ? from + per : last + 1;
+  auto add = [&](uint32_t i, int which) {
+    float x[8];
+    OpRaw<float> o;
+    o.load(a.part + ((size_t)i * 2 + which) * a.part_ld + c, 8);
+    o.get(x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] += x[k];
+  };
+  if (c < a.width) {
+    if (group == 0) add(piece, 1);
+    for (uint32_t i = from; i < to; ++i) add(i, 0);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sums[threadIdx.x][k] = acc[k];
+  __syncthreads();
+  if (group != 0 || c >= a.width) return;
+  for (int g = 1; g < groups; ++g)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] += sums[(g << p.shift) + lane][k];
+  grad_put(a, v, c, acc);
+}
+
+}  // namespace
+
+hipError_t fade_embed_launch(const OpTokens &t, size_t n, const OpMat &table, size_t vocab, size_t width, float scale, const OpMat &out, hipStream_t s) {
+  const int shift = lanes_shift(width, 8), rows = 256 >> shift;
+  const dim3 grid((uint32_t)((n + rows - 1) / rows));
+  auto go = [&](auto *in, auto *to) {
+    typedef std::remove_const_t<std::remove_pointer_t<decltype(in)>> TT;
+    typedef std::remove_pointer_t<decltype(to)> TO;
+    hipLaunchKernelGGL((embed_kernel<TT, TO>), grid, dim3(256), 0, s, t, n, in, table.ld, (uint32_t)vocab, (int)width, scale, to, out.ld, shift);
+  };
+  const float *tf = static_cast<const float *>(table.p);
+  const bf16_t *tb = static_cast<const bf16_t *>(table.p);
+  float *of = static_cast<float *>(const_cast<void *>(out.p));
+  bf16_t *ob = static_cast<bf16_t *>(const_cast<void *>(out.p));
+  if (table.f32 && out.f32) go(tf, of);
+  else if (table.f32) go(tf, ob);
+  else if (out.f32) go(tb, of);
+  else go(tb, ob);
+  return hipGetLastError();
+}
+
+size_t fade_embed_grad_bytes(size_t n, size_t vocab, size_t width) {
+  const GradPlan p = grad_plan(n, vocab, width);
+  return (size_t)p.pieces * p.strips > 0x7fffffff ? 0 : p.bytes;
+}
+
+hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout, float scale, float *grad, size_t grad_ld, size_t vocab, size_t width,
+                                  bool accumulate, void *work, hipStream_t s) {
+  const GradPlan p = grad_plan(n, vocab, width);
+  uint8_t *w = static_cast<uint8_t *>(work);
+  auto words = [&](size_t at) { return reinterpret_cast<uint32_t *>(w + at); };
+  uint32_t *hist = words(p.hist), *total = words(p.total), *k0 = words(p.keys[0]), *p0 = words(p.pos[0]), *k1 = words(p.keys[1]), *p1 = words(p.pos[1]);
+  uint8_t *flags = w + p.flags;
+  const dim3 tiles(p.tiles), scans(((1u << p.bits) + 3) / 4), b(256);
+  if (n == 0 && accumulate) return hipSuccess;
+  hipLaunchKernelGGL(sort_count_kernel<true>, tiles, b, 0, s, t, p, nullptr, nullptr, hist, flags, 0);
+  if (n) {
+    hipLaunchKernelGGL(sort_scan_kernel, scans, b, 0, s, p, hist, total);
+    if (p.passes == 1) {
+      hipLaunchKernelGGL((sort_place_kernel<true, true>), tiles, b, 0, s, t, p, nullptr, nullptr, hist, total, k0, p0, flags, 0);
+    } else {
+      hipLaunchKernelGGL((sort_place_kernel<true, false>), tiles, b, 0, s, t, p, nullptr, nullptr, hist, total, k1, p1, flags, 0);
+      hipLaunchKernelGGL(sort_count_kernel<false>, tiles, b, 0, s, t, p, k1, total, hist, flags, p.bits);
+      hipLaunchKernelGGL(sort_scan_kernel, scans, b, 0, s, p, hist, total);
+      hipLaunchKernelGGL((sort_place_kernel<false, true>), tiles, b, 0, s, t, p, k1, p1, hist, total, k0, p0, flags, p.bits);
+    }
+  }
+  const int groups = 256 >> p.shift;
+  if (!accumulate)
+    hipLaunchKernelGGL(grad_clear_kernel, dim3((uint32_t)((vocab + groups - 1) / groups)), b, 0, s, p, flags, grad, grad_ld, (int)width);
+  if (n) {
+    SumArgs a{k0, p0, total, dout.p, dout.ld, scale, grad, grad_ld, reinterpret_cast<float *>(w + p.part), (int)width, (int)((width + 7) & ~(size_t)7), accumulate};
+    const dim3 sums((uint32_t)(((size_t)p.pieces * p.strips + groups - 1) / groups));
+    if (dout.f32) hipLaunchKernelGGL(grad_sum_kernel<float>, sums, b, 0, s, p, a);
+    else hipLaunchKernelGGL(grad_sum_kernel<bf16_t>, sums, b, 0, s, p, a);
+    if (p.pieces > 1) hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)((size_t)p.pieces * p.strips)), b, 0, s, p, a);
+  }
+  return hipGetLastError();
+}
