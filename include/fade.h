@@ -189,7 +189,8 @@ int fade_coder_encode_tables_noalloc(fade_ctx *ctx, const uint16_t *freq_dev, co
  * atomics on floats), as a decoder that repeats an encoder's training needs. The current device of the calling thread is left as it was.
  *   - Matrices are row-major with `*_ld` elements from row to row (at least the width). Elements are FADE_F32 or FADE_BF16 by the
  *     `*_type` argument, on addresses that are multiples of the element's size; sums and statistics are fp32. Outputs may not overlap inputs
- *     or one another except where a call says so. Elements between the width and the ld are neither read nor written.
+ *     or one another except where a call says so. Elements between the width and the ld are not written, and
+ *     what they hold changes nothing.
  *   - Row counts are below 2^31. With no rows only parameter gradients are written (zeros, or left alone when accumulating),
  *     and pointers to rows may be NULL.
  *   - `work_dev`: scratch of at least the bytes that the call's *_work function gives, aligned to 16 bytes, contents undefined. Calls that can

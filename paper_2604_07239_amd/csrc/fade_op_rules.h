@@ -3,6 +3,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 namespace fade_op {
 
 struct GradPlan {
@@ -51,25 +53,32 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
   return p;
 }
 
-constexpr int WT = 128;  // tile of a weight gradient: WT x WT on four wavefronts
+// The weight gradient K x N over `rows` rows: tiles of the result, and equal ranges of the rows (units of 64) whose sums are added up behind it.
 struct WgradPlan {
+  bool large;  // tiles of 256 x 256 (fp32 dy: 256 x 128), one workgroup of eight wavefronts per compute unit; else 128 x 128
   int tiles_m, tiles_n, units, ranges, per;
 };
-// Ranges of the rows: as many as fill the chip where the tiles do not, and so many that no fp32 sum runs over more than 16384 products' worth
-// of rows (4096 where three terms each are added).
 inline WgradPlan wgrad_plan(size_t rows, size_t K, size_t N, bool f32) {
-  WgradPlan p{};
-  p.tiles_m = (int)((K + WT - 1) / WT);
-  p.tiles_n = (int)((N + WT - 1) / WT);
-  p.units = (int)((rows + 63) / 64);
-  const size_t tiles = (size_t)p.tiles_m * p.tiles_n, chain = f32 ? 64 : 256;
-  size_t r = tiles >= 512 ? 1 : 512 / tiles;
-  if (r > (size_t)p.units) r = p.units;
-  if (r < (p.units + chain - 1) / chain) r = (p.units + chain - 1) / chain;
-  r = r < 1 ? 1 : r > 1024 ? 1024 : r;
-  p.per = (int)((p.units + r - 1) / r);
-  p.ranges = p.per ? (p.units + p.per - 1) / p.per : 1;
-  return p;
+  const size_t units = (rows + 63) / 64, chain = f32 ? 64 : 256;  // units that one fp32 sum may run over
+  WgradPlan best{};
+  double least = 0;
+  for (const bool large : {true, false}) {
+    const size_t bm = large ? 256 : 128, bn = large && !f32 ? 256 : 128, tm = (K + bm - 1) / bm, tn = (N + bn - 1) / bn, tiles = tm * tn;
+    for (size_t want = 1; want <= 1024 && (want == 1 || want <= units); want += want < 8 ? 1 : want / 4) {
+      const size_t per = (units + want - 1) / want, r = per ? (units + per - 1) / per : 1;  // no range is empty
+      if (per > chain && want + want / 4 <= 1024) continue;
+      // cost in microseconds
+      const size_t at_once = 256 * (large || f32 ? 1 : 2), rounds = (tiles * r + at_once - 1) / at_once;
+      const double unit = (large ? (f32 ? 2.7 : 1.8) : (f32 ? 1.4 : 1.0)), add = r > 1 ? 3.0 + (double)(r + r + 1) * K * N * 4 / 4e6 : 0.0;
+      const double cost = rounds * (per * unit + 3.0) + add;
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = WgradPlan{large, (int)tm, (int)tn, (int)units, (int)r, (int)per};
+      }
+      if (tiles * r > 4 * 256 && per <= chain) break;
+    }
+  }
+  return best;
 }
 
 // Lanes for a row: 8 columns each, from 16 to a workgroup of 1024; two steps of 8 columns above 8192.
