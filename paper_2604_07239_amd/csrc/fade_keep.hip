@@ -72,18 +72,30 @@ __device__ __forceinline__ void wg_split(float v, uint32_t &hi, uint32_t &mid, u
   lo = __builtin_bit_cast(uint32_t, rest - __builtin_bit_cast(float, mid));
 }
 __device__ __forceinline__ uint32_t wg_upper(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }  // upper halves, a's first
-__device__ __forceinline__ bf16x8 wg_widen(uint32_t lo, uint32_t hi, float unit) {
-  float v[8];
-  op_keep_unpack(make_uint2(lo, hi), unit, v);
+// 8 bytes of a checkpoint as bf16, exactly: as unsigned bytes 128 too large, which one instruction each converts, then unit * byte - 128 unit
+__device__ __forceinline__ bf16x8 wg_widen(uint32_t lo, uint32_t hi, uint32_t e) {
+  const float unit = op_keep_unit(e), bias = -128.0f * unit;
+  lo ^= 0x80808080u;
+  hi ^= 0x80808080u;
   bf16x8 b;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) b[k] = (bf16_t)v[k];
+  for (int k = 0; k < 8; ++k) b[k] = (bf16_t)fmaf((float)(((k < 4 ? lo : hi) >> ((k & 3) * 8)) & 0xffu), unit, bias);
   return b;
 }
 
+// MM matrix instructions, between them evenly RD reads of LDS, WR writes and VA vector instructions, as the compiler is told to order them
+template <int MM, int RD, int WR, int VA, int K = 0> __device__ __forceinline__ void wg_pace() {
+  if constexpr (K < MM) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (RD * (K + 1) / MM > RD * K / MM) __builtin_amdgcn_sched_group_barrier(0x100, RD * (K + 1) / MM - RD * K / MM, 0);
+    if constexpr (VA * (K + 1) / MM > VA * K / MM) __builtin_amdgcn_sched_group_barrier(0x002, VA * (K + 1) / MM - VA * K / MM, 0);
+    if constexpr (WR * (K + 1) / MM > WR * K / MM) __builtin_amdgcn_sched_group_barrier(0x200, WR * (K + 1) / MM - WR * K / MM, 0);
+    wg_pace<MM, RD, WR, VA, K + 1>();
+  }
+}
 // WM x WN wavefronts, each TM x TN tiles of 32 x 32. Units of 64 rows pass through two places in LDS: while the matrix cores work on one, the
 // next is on its way through the registers (x has to be widened, an fp32 dy split, on the way) into the other; one barrier a unit.
-template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__(WM *WN * 64, 1) void keep_grad_kernel(WgradArgs g) {
+template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__(WM * WN * 64, 1) void keep_grad_kernel(WgradArgs g) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NT = WM * WN * 64, PLANES = F32 ? 3 : 1;
   constexpr int A_BYTES = 64 * BM * 2, B_BYTES = 64 * BN * 2, PLACE = A_BYTES + PLANES * B_BYTES;
   constexpr int QA = 64 * BM / 16 / NT, QB = 64 * BN / 8 / NT;  // 16 columns of x, 8 of dy: pieces per thread and unit
@@ -110,83 +122,80 @@ template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__
   };
 
   const size_t pitch = (size_t)g.x.groups * 32;
-  const uint8_t *exps = g.x.p + g.x.rows * pitch;
   typedef std::conditional_t<F32, float, bf16_t> TD;
-  const TD *dy = static_cast<const TD *>(g.dy);
-  // this thread's pieces. Columns that do not exist read column 0: what they bring reaches only results that do not exist.
-  int xr[QA], xc[QA], yr[QB], yc[QB];
-#pragma unroll
-  for (int i = 0; i < QA; ++i) {
-    xr[i] = (tid + i * NT) / (BM / 16);
-    xc[i] = (tid + i * NT) % (BM / 16);
-  }
-#pragma unroll
-  for (int i = 0; i < QB; ++i) {
-    yr[i] = (tid + i * NT) / (BN / 8);
-    yc[i] = (tid + i * NT) % (BN / 8);
-  }
+  // This thread's pieces: where they go in a place, and where the unit's come from, as an offset from the unit's first row; its pieces are XS (YS) rows
+  // apart, multiples of 4, so the others follow from the first. Columns that do not exist read column 0: what they bring reaches only results that do not exist.
+  constexpr int XS = NT / (BM / 16), YS = NT / (BN / 8);
+  static_assert(XS % 4 == 0 && YS % 4 == 0, "the permutation of a piece's row");
+  const int xr = tid / (BM / 16), xc = tid % (BM / 16), xcol = m0 + xc * 16 < (int)pitch ? m0 + xc * 16 : 0;
+  const int yr = tid / (BN / 8), yc = n0 + tid % (BN / 8) * 8, ycol = yc < g.N ? yc : 0;
+  const int x_at = piece_at(BM * 2, xr, xc * 2), y_at = A_BYTES + piece_at(BN * 2, yr, tid % (BN / 8));
+  const uint32_t x_off = (uint32_t)xr * (uint32_t)pitch + xcol, e_off = (uint32_t)xr * g.x.groups + (xcol >> 5);
+  const uint32_t y_off = (uint32_t)yr * (uint32_t)g.dy_ld + ycol;
+  const uint8_t *x_row = g.x.p + (size_t)u0 * 64 * pitch, *e_row = g.x.p + g.x.rows * pitch + (size_t)u0 * 64 * g.x.groups;
+  const TD *y_row = static_cast<const TD *>(g.dy) + (size_t)u0 * 64 * g.dy_ld;
   uint4 qx[QA];
   uint32_t ex[QA];
   OpRaw<TD> qy[QB];
   // The last unit, whose rows may end and whose last piece of dy may reach past the matrix, is loaded with every access checked. In the others a piece that
   // starts in a row ends in the next one at the latest (rows of 8 columns or more), which exists.
-  auto load = [&](int u) {
+  auto load = [&](int u) {  // units in order
     if (u + 1 < g.units && g.N >= 8) {
 #pragma unroll
       for (int i = 0; i < QA; ++i) {
-        const size_t row = (size_t)u * 64 + xr[i], c = (size_t)(m0 + xc[i] * 16) < pitch ? m0 + xc[i] * 16 : 0;
-        qx[i] = *reinterpret_cast<const uint4 *>(g.x.p + row * pitch + c);
-        ex[i] = exps[row * g.x.groups + (c >> 5)];
+        qx[i] = *reinterpret_cast<const uint4 *>(x_row + i * XS * pitch + x_off);
+        ex[i] = (e_row + (size_t)i * XS * g.x.groups)[e_off];
       }
 #pragma unroll
-      for (int i = 0; i < QB; ++i) {
-        const size_t row = (size_t)u * 64 + yr[i], c = n0 + yc[i] * 8 < g.N ? n0 + yc[i] * 8 : 0;
-        qy[i].load(dy + row * g.dy_ld + c, 8);
-      }
+      for (int i = 0; i < QB; ++i) qy[i].load(y_row + i * YS * g.dy_ld + y_off, 8);
     } else {
+      const int left = (int)(g.x.rows - (size_t)u * 64 < 64 ? g.x.rows - (size_t)u * 64 : 64);
 #pragma unroll
       for (int i = 0; i < QA; ++i) {
-        const size_t row = (size_t)u * 64 + xr[i], c = m0 + xc[i] * 16;
         qx[i] = make_uint4(0, 0, 0, 0);
         ex[i] = 0;
-        if (row < g.x.rows && c < pitch) {
-          qx[i] = *reinterpret_cast<const uint4 *>(g.x.p + row * pitch + c);
-          ex[i] = exps[row * g.x.groups + (c >> 5)];
+        if (xr + i * XS < left) {
+          qx[i] = *reinterpret_cast<const uint4 *>(x_row + i * XS * pitch + x_off);
+          ex[i] = (e_row + (size_t)i * XS * g.x.groups)[e_off];
         }
       }
 #pragma unroll
       for (int i = 0; i < QB; ++i) {
-        const size_t row = (size_t)u * 64 + yr[i];
-        const int c = n0 + yc[i] * 8;
         qy[i].zero();
-        if (row < g.x.rows && c < g.N) qy[i].load(dy + row * g.dy_ld + c, g.N - c);
+        if (yr + i * YS < left && yc < g.N) qy[i].load(y_row + i * YS * g.dy_ld + y_off, g.N - yc);
       }
     }
+    x_row += pitch * 64;
+    e_row += (size_t)g.x.groups * 64;
+    y_row += g.dy_ld * 64;
   };
-  auto store = [&](uint8_t *to) {
+  // what has been loaded, into a place: a quarter at each step (bf16), or all of it at the third (fp32, whose splitting the compiler spreads better by itself)
+  auto store = [&](uint8_t *to, int quarter) {
+    if (F32 && quarter != 2) return;
 #pragma unroll
-    for (int i = 0; i < QA; ++i) {
-      const float unit = op_keep_unit(ex[i]);
-      *reinterpret_cast<bf16x8 *>(to + piece_at(BM * 2, xr[i], xc[i] * 2)) = wg_widen(qx[i].x, qx[i].y, unit);
-      *reinterpret_cast<bf16x8 *>(to + piece_at(BM * 2, xr[i], xc[i] * 2 + 1)) = wg_widen(qx[i].z, qx[i].w, unit);
-    }
-#pragma unroll
-    for (int i = 0; i < QB; ++i) {
-      uint8_t *dst = to + A_BYTES + piece_at(BN * 2, yr[i], yc[i]);
-      if constexpr (F32) {
-        float v[8];
-        qy[i].get(v);
-        uint32_t w[3][8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) wg_split(v[k], w[0][k], w[1][k], w[2][k]);
-#pragma unroll
-        for (int t = 0; t < 3; ++t)
-          *reinterpret_cast<uint4 *>(dst + t * B_BYTES) = make_uint4(wg_upper(w[t][0], w[t][1]), wg_upper(w[t][2], w[t][3]), wg_upper(w[t][4], w[t][5]),
-                                                                     wg_upper(w[t][6], w[t][7]));
-      } else {
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(qy[i].v[0], qy[i].v[1], qy[i].v[2], qy[i].v[3]);
+    for (int h = 0; h < 2 * QA; ++h)
+      if (F32 || h * 4 / (2 * QA) == quarter) {  // an even piece's neighbour is its neighbour after the permutation too
+        uint32_t lo = h % 2 ? qx[h / 2].z : qx[h / 2].x, hi = h % 2 ? qx[h / 2].w : qx[h / 2].y;
+        if constexpr (!F32) asm volatile("" : "+v"(lo), "+v"(hi));  // its quarter's work stays among its quarter's matrix instructions
+        *reinterpret_cast<bf16x8 *>(to + x_at + h / 2 * XS * BM * 2 + h % 2 * 16) = wg_widen(lo, hi, ex[h / 2]);
       }
-    }
+#pragma unroll
+    for (int i = 0; i < QB; ++i)
+      if (F32 || i * 4 / QB == quarter) {
+        if constexpr (F32) {
+          float v[8];
+          qy[i].get(v);
+          uint32_t w[3][8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) wg_split(v[k], w[0][k], w[1][k], w[2][k]);
+#pragma unroll
+          for (int t = 0; t < 3; ++t)
+            *reinterpret_cast<uint4 *>(to + y_at + i * YS * BN * 2 + t * B_BYTES) = make_uint4(wg_upper(w[t][0], w[t][1]), wg_upper(w[t][2], w[t][3]),
+                                                                                wg_upper(w[t][4], w[t][5]), wg_upper(w[t][6], w[t][7]));
+        } else {
+          *reinterpret_cast<uint4 *>(to + y_at + i * YS * BN * 2) = make_uint4(qy[i].v[0], qy[i].v[1], qy[i].v[2], qy[i].v[3]);
+        }
+      }
   };
   f32x16 acc[TM][TN];
 #pragma unroll
@@ -195,35 +204,67 @@ template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  auto multiply = [&](const uint8_t *from, int ks) {
-    bf16x8 a[TM], b[TN];
+  // operands of one step of 16 rows, read a step ahead of the matrix instructions
+  bf16x8 a[2][TM], b[2][PLANES][TN];
+  auto read = [&](int buf, const uint8_t *from, int ks) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) a[i] = turned(from, BM * 2, wm * TM + i, ks);
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int t = PLANES - 1; t >= 0; --t) {  // the smallest terms first
+      for (int t = PLANES - 1; t >= 0; --t) b[buf][t][j] = turned(from + A_BYTES + t * B_BYTES, BN * 2, wn * TN + j, ks);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) b[j] = turned(from + A_BYTES + t * B_BYTES, BN * 2, wn * TN + j, ks);
+    for (int i = 0; i < TM; ++i) a[buf][i] = turned(from, BM * 2, wm * TM + i, ks);
+  };
+  auto multiply = [&](int buf) {
+#pragma unroll
+    for (int t = PLANES - 1; t >= 0; --t)  // the smallest terms first
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
-    }
+        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[buf][i], b[buf][t][j], acc[i][j], 0, 0, 0);
+  };
+  // a step's matrix instructions, and between them the next step's reads and a quarter of the next unit's way into LDS
+  constexpr int MM = PLANES * TM * TN, RD = 2 * (TM + PLANES * TN), WR = F32 ? 0 : QA / 2 + QB / 4, VA = F32 ? 0 : QA / 2 * 24;
+  auto hand_over = [] {  // this wavefront's LDS accesses are done; then everybody's
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
 
   if (u0 < u1) {
+    uint8_t *here = smem, *next = smem + PLACE;
     load(u0);
-    store(smem);
-    __syncthreads();
-    for (int u = u0; u < u1; ++u) {
-      uint8_t *here = smem + ((u - u0) & 1) * PLACE, *next = smem + ((u - u0 + 1) & 1) * PLACE;
-      if (u + 1 < u1) load(u + 1);
-      multiply(here, 0);
-      multiply(here, 1);
-      multiply(here, 2);
-      if (u + 1 < u1) store(next);
-      multiply(here, 3);
-      __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) store(here, k);
+    if (u0 + 1 < u1) load(u0 + 1);
+    hand_over();
+    read(0, here, 0);
+    for (int u = u0; u + 1 < u1; ++u) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        read((k + 1) & 1, here, k + 1);
+        store(next, k);
+        multiply(k & 1);
+        if (!F32 || k < 2) wg_pace<MM, RD, WR, VA>();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      store(next, 3);
+      if (u + 2 < u1) load(u + 2);
+      hand_over();
+      read(0, next, 0);
+      multiply(1);
+      wg_pace<MM, RD, 0, 0>();
+      uint8_t *t = here;
+      here = next;
+      next = t;
     }
+    read(1, here, 1);
+    multiply(0);
+    read(0, here, 2);
+    multiply(1);
+    read(1, here, 3);
+    multiply(0);
+    multiply(1);
   }
   // a lane holds a column of each 32 x 32 tile: runs of 128 bytes
   float *out = g.out + (size_t)range * g.K * g.out_ld;
@@ -242,14 +283,48 @@ template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__
       }
     }
 }
-// the ranges' sums, added in their order
-__global__ __launch_bounds__(256) void keep_grad_add_kernel(const float *part, int ranges, int K, int N, float *grad, size_t ld, bool add) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, count = (size_t)K * N;
-  if (i >= count) return;
-  float s = 0.0f;
-  for (int r = 0; r < ranges; ++r) s += part[(size_t)r * count + i];
-  float *dst = grad + i / N * ld + i % N;
-  *dst = add ? *dst + s : s;
+// The ranges' sums, added in their order, V pieces of four values per thread: a gradient without gaps between its rows is one run of values; else a
+// workgroup takes 1024 V columns of a row.
+template <int V>
+__global__ __launch_bounds__(256) void keep_grad_add_kernel(const float *part, int ranges, size_t count, int N, int blocks_n, float *grad, size_t ld, bool add) {
+  size_t row = 0, first = (size_t)blockIdx.x * (1024 * V), have = count;
+  if (blocks_n) {
+    row = blockIdx.x / blocks_n;
+    first = (blockIdx.x - row * blocks_n) * (1024 * V);
+    have = N;
+  }
+  const float *src = part + row * N + first;
+  float *dst = grad + row * ld + first;
+  const int left = have - first < 1024 * V ? (int)(have - first) : 1024 * V, at = threadIdx.x * 4;
+  op_f32x4 s[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) s[k] = op_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (left == 1024 * V) {  // all of them are there: loads of several ranges at once
+    constexpr int AHEAD = 8 / V;
+#pragma unroll AHEAD
+    for (int r = 0; r < ranges; ++r, src += count)
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[k] += *reinterpret_cast<const op_f32x4 *>(src + at + k * 1024);
+  } else {
+    for (int r = 0; r < ranges; ++r, src += count)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at + k * 1024 + i < left) s[k][i] += src[at + k * 1024 + i];
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int c = at + k * 1024;
+    if (c + 4 <= left) {
+      op_f32x4 *to = reinterpret_cast<op_f32x4 *>(dst + c);
+      *to = add ? *to + s[k] : s[k];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (c + i < left) dst[c + i] = add ? dst[c + i] + s[k][i] : s[k][i];
+    }
+  }
 }
 
 }  // namespace
@@ -296,11 +371,16 @@ hipError_t fade_keep_grad_launch(const OpKeep &k, size_t in_width, const OpMat &
   const bool parts = p.ranges > 1;
   const WgradArgs g{k, dy.p, dy.ld, (int)in_width, (int)out_width, p.tiles_m, p.tiles_n, p.ranges, p.units, p.per, parts ? static_cast<float *>(work) : grad,
                     parts ? out_width : grad_ld, !parts && accumulate};
-  const hipError_t e = dy.f32 ? (p.large ? wgrad_go<4, 2, 2, 2, true>(g, s) : wgrad_go<2, 2, 2, 2, true>(g, s))
-                              : (p.large ? wgrad_go<2, 4, 4, 2, false>(g, s) : wgrad_go<2, 2, 2, 2, false>(g, s));
+  const hipError_t e = dy.f32 ? (p.large ? wgrad_go<4, 2, 2, 2, true>(g, s) : wgrad_go<2, 4, 2, 1, true>(g, s))
+                              : (p.large ? wgrad_go<2, 4, 4, 2, false>(g, s) : wgrad_go<2, 4, 2, 1, false>(g, s));
   if (e != hipSuccess) return e;
-  if (parts)
-    hipLaunchKernelGGL(keep_grad_add_kernel, dim3((uint32_t)((in_width * out_width + 255) / 256)), dim3(256), 0, s, static_cast<const float *>(work),
-                       p.ranges, (int)in_width, (int)out_width, grad, grad_ld, accumulate);
+  if (parts) {
+    const size_t count = in_width * out_width;
+    const bool gaps = grad_ld != out_width, four = count >= (size_t)1 << 22;  // pieces enough for every compute unit
+    const size_t block = four ? 4096 : 1024, wide = (out_width + block - 1) / block;
+    const dim3 grid((uint32_t)(gaps ? in_width * wide : (count + block - 1) / block));
+    auto *f = four ? keep_grad_add_kernel<4> : keep_grad_add_kernel<1>;
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, s, static_cast<const float *>(work), p.ranges, count, (int)out_width, gaps ? (int)wide : 0, grad, grad_ld, accumulate);
+  }
   return hipGetLastError();
 }

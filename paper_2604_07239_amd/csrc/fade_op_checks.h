@@ -9,7 +9,7 @@
 
 namespace fade_op {
 
-constexpr size_t ROWS = 0x7fffffff, WIDTH = (size_t)1 << 20, VOCAB = (size_t)1 << 20, GRAD_WIDTH = 65536, JOIN_WIDTH = 16384;
+constexpr size_t ROWS = 0x7fffffff, WIDTH = (size_t)1 << 20, VOCAB = (size_t)1 << 20, GRAD_WIDTH = 65536, GRAD_LD = (size_t)1 << 22, JOIN_WIDTH = 16384;
 
 inline bool type(uint32_t t) { return t == FADE_F32 || t == FADE_BF16; }
 inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -53,7 +53,7 @@ inline const char *weight_grad(const void *k, size_t rows, size_t in_width, cons
   if (!grad_sizes(rows, in_width, out_width) || need == 0) return "rows or widths out of range";
   if (!type(dy_type)) return "unknown type";
   if (!keep(k, rows)) return "checkpoint missing or not aligned to 16 bytes";
-  if (!matrix(dy, dy_type, rows, out_width, dy_ld)) return "dy";
+  if (!matrix(dy, dy_type, rows, out_width, dy_ld) || dy_ld > GRAD_LD) return "dy";
   if (!matrix(grad, FADE_F32, in_width, out_width, grad_ld)) return "grad";
   return work(w, have, need) ? nullptr : "workspace missing, too small or not aligned to 16 bytes";
 }

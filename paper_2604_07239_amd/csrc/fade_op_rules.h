@@ -54,12 +54,19 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
 }
 
 // The weight gradient K x N over `rows` rows: tiles of the result, and equal ranges of the rows (units of 64) whose sums are added up behind it.
+// Of tile sizes and counts of ranges the cheapest by a model of what was measured, in us: 256 x 256 tiles (fp32 dy: 256 x 128) take 1.85 (2.75) a unit with one
+// workgroup per compute unit, 128 x 128 tiles 0.72 (1.6), or 1.45 with two of them; the first loads and the last stores 10 and 4; sums leave at 5.5 MB/us, and
+// the launch that adds several takes 4.5 more. Measured, the rule's choice | others: 16384 rows, 4096 x 2048, bf16 276 (large, 2) | 420 (large, 1), 364 (small, 1);
+// 4096 rows, 1024 x 1024 26.2 (small, 4) | 34 (2), 28.6 (8), 34.5 (large, 8); 512 rows, 512 x 512 9.6 (small, 1) | 9.7 (2), 17.9 (large, 4); fp32, 16384 rows,
+// 2048 x 2048 383 (large, 2) | 416 (small, 1); 1500 rows, 512 x 1000 18.8 (small, 6) | 19.4 (4), 23.7 (large, 8).
+// A sum over thousands of rows in one fp32 accumulator drifts with its length: no range is longer than 16384 rows, 4096 with fp32 dy's three products a
+// row, until there are 1024 ranges.
 struct WgradPlan {
-  bool large;  // tiles of 256 x 256 (fp32 dy: 256 x 128), one workgroup of eight wavefronts per compute unit; else 128 x 128
-  int tiles_m, tiles_n, units, ranges, per;
+  bool large;
+  int tiles_m, tiles_n, units, ranges, per;  // units of 64 rows; units in one range
 };
 inline WgradPlan wgrad_plan(size_t rows, size_t K, size_t N, bool f32) {
-  const size_t units = (rows + 63) / 64, chain = f32 ? 64 : 256;  // units that one fp32 sum may run over
+  const size_t units = (rows + 63) / 64, chain = f32 ? 64 : 256;
   WgradPlan best{};
   double least = 0;
   for (const bool large : {true, false}) {
@@ -67,15 +74,15 @@ inline WgradPlan wgrad_plan(size_t rows, size_t K, size_t N, bool f32) {
     for (size_t want = 1; want <= 1024 && (want == 1 || want <= units); want += want < 8 ? 1 : want / 4) {
       const size_t per = (units + want - 1) / want, r = per ? (units + per - 1) / per : 1;  // no range is empty
       if (per > chain && want + want / 4 <= 1024) continue;
-      // cost in microseconds
-      const size_t at_once = 256 * (large || f32 ? 1 : 2), rounds = (tiles * r + at_once - 1) / at_once;
-      const double unit = (large ? (f32 ? 2.7 : 1.8) : (f32 ? 1.4 : 1.0)), add = r > 1 ? 3.0 + (double)(r + r + 1) * K * N * 4 / 4e6 : 0.0;
-      const double cost = rounds * (per * unit + 3.0) + add;
+      const bool pair = !large && !f32 && tiles * r > 256;
+      const double unit = large ? (f32 ? 2.75 : 1.85) : f32 ? 1.6 : pair ? 1.45 : 0.72, bytes = 4.0 * K * N;
+      const size_t rounds = (tiles * r + (pair ? 511 : 255)) / (pair ? 512 : 256);
+      const double cost = (large ? 10.0 : 4.0) + rounds * per * unit + r * bytes / 5.5e6 + (r > 1 ? 4.5 + (r + 1) * bytes / 5.5e6 : 0.0);
       if (least == 0 || cost < least) {
         least = cost;
         best = WgradPlan{large, (int)tm, (int)tn, (int)units, (int)r, (int)per};
       }
-      if (tiles * r > 4 * 256 && per <= chain) break;
+      if (tiles * r > 1024 && per <= chain) break;  // more ranges only add sums
     }
   }
   return best;
