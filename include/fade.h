@@ -233,7 +233,7 @@ int fade_checkpoint_weight_grad(fade_ctx *ctx, const void *keep_dev, size_t rows
  * Eq. 9-10, for any program's block), per row of `width` columns:
  *     z = N_u(u),   h = lam * r + sigma(g) * z,   n = N_n(h)
  * N_u, N_n: FADE_NORM_NONE (the identity), FADE_NORM_LAYER ((x - mean) / sqrt(var + eps) * gamma + beta, biased variance) or FADE_NORM_RMS
- * (x / sqrt(mean(x^2) + eps) * gamma + beta). n is formed from h before h is rounded. `width` is at most 16384.
+ * (x / sqrt(mean(x^2) + eps) * gamma + beta). n is formed from h before h is rounded. `width` is at most 8192.
  * The backward pass takes r, u and g again, as they were or as checkpoints of them, forms the statistics anew, and gives, for the gradients
  * dh (through later uses of h) and dn, those of r, u, g and of the parameters. */
 enum { FADE_NORM_NONE = 0, FADE_NORM_LAYER = 1, FADE_NORM_RMS = 2 };

@@ -65,32 +65,29 @@ template <int L> struct RowSums {
 };
 
 // statistics of a row's values x: mean (0 unless LayerNorm) and 1 / sigma
-template <int V, int L> __device__ __forceinline__ void row_stats(RowSums<L> &rs, int norm, const float (&x)[V][8], const int (&left)[V], float mine, float C,
-                                                                  float eps, float &mean, float &rstd) {
+template <int L>
+__device__ __forceinline__ void row_stats(RowSums<L> &rs, int norm, const float (&x)[8], int left, float mine, float C, float eps, float &mean, float &rstd) {
   float sq;
   if (norm == FADE_NORM_LAYER) {
     float s = 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s += x[v][k];  // columns that do not exist hold zeros
+    for (int k = 0; k < 8; ++k) s += x[k];  // columns that do not exist hold zeros
     rs.moments(s, mine, C, mean, sq, [&](float m) {
       float q = 0.0f;
+      if (left >= 8) {
 #pragma unroll
-      for (int v = 0; v < V; ++v)
+        for (int k = 0; k < 8; ++k) q = fmaf(x[k] - m, x[k] - m, q);
+      } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float d = k < left[v] ? x[v][k] - m : 0.0f;
-          q = fmaf(d, d, q);
-        }
+        for (int k = 0; k < 7; ++k)
+          if (k < left) q = fmaf(x[k] - m, x[k] - m, q);
+      }
       return q;
     });
   } else {
     float q[1] = {0.0f};
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) q[0] = fmaf(x[v][k], x[v][k], q[0]);
+    for (int k = 0; k < 8; ++k) q[0] = fmaf(x[k], x[k], q[0]);
     rs.sum(q);
     mean = 0.0f;
     sq = q[0];
@@ -109,116 +106,118 @@ __device__ __forceinline__ void param8(const float *p, float otherwise, int c, i
     r.get(x);
   }
 }
+// A parameter's columns of this lane: held in registers over all the rows, or, on rows of 1024 lanes, whose workgroup has 128 registers a lane, fetched
+// from the caches at each use.
+template <bool HELD> struct Param {
+  const float *p;
+  float otherwise, held[HELD ? 8 : 1];
+  int c, left;
+  __device__ __forceinline__ Param(const float *p_, float o, int c_, int left_) : p(p_), otherwise(o), c(c_), left(left_) {
+    if constexpr (HELD) param8(p, otherwise, c, left, held);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    if constexpr (HELD) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = held[k];
+    } else {
+      param8(p, otherwise, c, left, x);
+    }
+  }
+};
 // sigma(x) = 1 / (1 + exp(-x)); fade_sigmoid's reciprocal is the hardware's, good to an ulp
 __device__ __forceinline__ float sigma(float x) { return fade_sigmoid(x); }
 
-template <int L, int V> struct Lanes {
-  int group, lane, c[V], left[V];
+template <int L> struct Lane {
+  int group, lane, c, left;
   float mine;  // columns of this wavefront (of this row where a wavefront holds several)
-  __device__ __forceinline__ Lanes(int width) {
+  __device__ __forceinline__ Lane(int width) {
     group = threadIdx.x / L;
     lane = threadIdx.x % L;
-    int n = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      c[v] = (v * L + lane) * 8;
-      left[v] = width - c[v];
-      const int first = (v * L + (L > 64 ? lane / 64 * 64 : 0)) * 8, have = width - first, span = (L < 64 ? L : 64) * 8;
-      n += have < 0 ? 0 : have > span ? span : have;
-    }
-    mine = (float)n;
+    c = lane * 8;
+    left = width - c;
+    const int have = width - (L > 64 ? lane / 64 * 512 : 0), span = (L < 64 ? L : 64) * 8;
+    mine = (float)(have < 0 ? 0 : have > span ? span : have);
   }
 };
 
-template <int V> __device__ __forceinline__ void keep_row(uint8_t *keep, int rows, int width, size_t row, bool in, const float (&x)[V][8], const int (&c)[V]) {
+__device__ __forceinline__ void keep_row(uint8_t *keep, int rows, int width, size_t row, bool in, const float (&x)[8], int c) {
   const int groups = (width + 31) / 32;
-  uint8_t *q = keep + row * groups * 32, *e = keep + (size_t)rows * groups * 32 + row * groups;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    uint32_t exp;
-    const uint2 w = op_keep_pack(x[v], exp);
-    if (in && c[v] < groups * 32) {
-      *reinterpret_cast<uint2 *>(q + c[v]) = w;
-      if ((threadIdx.x & 3) == 0) e[c[v] >> 5] = (uint8_t)exp;
-    }
+  uint32_t exp;
+  const uint2 w = op_keep_pack(x, exp);
+  if (in && c < groups * 32) {
+    *reinterpret_cast<uint2 *>(keep + row * groups * 32 + c) = w;
+    if ((threadIdx.x & 3) == 0) keep[(size_t)rows * groups * 32 + row * groups + (c >> 5)] = (uint8_t)exp;
   }
 }
 
-template <int L, int V, typename TS, typename TB> __global__ __launch_bounds__(most(L, 256)) void join_kernel(JoinArgs a) {
+// A workgroup takes rows in strides of the grid; the next rows' operands are on their way while it works on these.
+template <int L, typename TS, typename TB> __global__ __launch_bounds__(most(L, 256)) void join_kernel(JoinArgs a) {
   typedef RowSums<L> Sums;
+  typedef Param<(L <= 512)> P;
   __shared__ float lds[2][Sums::GROUPS][Sums::W > 0 ? Sums::W : 1][4];
-  const Lanes<L, V> l(a.width);
+  const Lane<L> l(a.width);
   Sums rs{lds, 0, l.group, l.lane / 64};
-  float gu[V][8], bu[V][8], gn[V][8], bn[V][8], lam[V][8];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    param8(a.gamma_u, 1.0f, l.c[v], l.left[v], gu[v]);
-    param8(a.beta_u, 0.0f, l.c[v], l.left[v], bu[v]);
-    param8(a.gamma_n, 1.0f, l.c[v], l.left[v], gn[v]);
-    param8(a.beta_n, 0.0f, l.c[v], l.left[v], bn[v]);
-    param8(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c[v], l.left[v], lam[v]);
-  }
+  const P gu(a.gamma_u, 1.0f, l.c, l.left), bu(a.beta_u, 0.0f, l.c, l.left), gn(a.gamma_n, 1.0f, l.c, l.left), bn(a.beta_n, 0.0f, l.c, l.left),
+      lam(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c, l.left);
   const float C = (float)a.width;
-  for (uint32_t base = blockIdx.x * Sums::GROUPS; base < (uint32_t)a.rows; base += gridDim.x * Sums::GROUPS) {
-    const bool in = base + l.group < (uint32_t)a.rows;  // the workgroup's barriers are for all its rows
-    const size_t row = in ? base + l.group : a.rows - 1;
-    OpRaw<TS> raw_r[V];
-    OpRaw<TB> raw_u[V], raw_g[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      raw_r[v].zero(); raw_u[v].zero(); raw_g[v].zero();
-      if (l.left[v] > 0) {
-        raw_r[v].load(static_cast<const TS *>(a.r) + row * a.r_ld + l.c[v], l.left[v]);
-        raw_u[v].load(static_cast<const TB *>(a.u) + row * a.u_ld + l.c[v], l.left[v]);
-        if (a.g) raw_g[v].load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c[v], l.left[v]);
-      }
+  OpRaw<TS> raw_r;
+  OpRaw<TB> raw_u, raw_g;
+  auto load = [&](size_t row) {
+    raw_r.zero(); raw_u.zero(); raw_g.zero();
+    if (row < (size_t)a.rows && l.left > 0) {
+      raw_r.load(static_cast<const TS *>(a.r) + row * a.r_ld + l.c, l.left);
+      raw_u.load(static_cast<const TB *>(a.u) + row * a.u_ld + l.c, l.left);
+      if (a.g) raw_g.load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c, l.left);
     }
-    float x[V][8], h[V][8], g[V][8];
-#pragma unroll
-    for (int v = 0; v < V; ++v) { raw_u[v].get(x[v]); raw_r[v].get(h[v]); raw_g[v].get(g[v]); }
-    if (a.keep_r) keep_row<V>(a.keep_r, a.rows, a.width, row, in, h, l.c);
-    if (a.keep_u) keep_row<V>(a.keep_u, a.rows, a.width, row, in, x, l.c);
-    if (a.keep_g) keep_row<V>(a.keep_g, a.rows, a.width, row, in, g, l.c);
+  };
+  uint32_t base = blockIdx.x * Sums::GROUPS;
+  load(base + l.group);
+  for (; base < (uint32_t)a.rows; base += gridDim.x * Sums::GROUPS) {
+    const size_t row = base + l.group;
+    const bool in = row < (size_t)a.rows;  // the workgroup's barriers are for all its rows
+    float x[8], h[8], g[8], p[8], q[8];
+    raw_u.get(x); raw_r.get(h); raw_g.get(g);
+    load(row + gridDim.x * Sums::GROUPS);
+    if (a.keep_r) keep_row(a.keep_r, a.rows, a.width, row, in, h, l.c);
+    if (a.keep_u) keep_row(a.keep_u, a.rows, a.width, row, in, x, l.c);
+    if (a.keep_g) keep_row(a.keep_g, a.rows, a.width, row, in, g, l.c);
     if (a.norm_u != FADE_NORM_NONE) {
       float mean, rstd;
-      row_stats<V>(rs, a.norm_u, x, l.left, l.mine, C, a.eps, mean, rstd);
+      row_stats(rs, a.norm_u, x, l.left, l.mine, C, a.eps, mean, rstd);
+      gu.get(p); bu.get(q);
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[v][k] = fmaf((x[v][k] - mean) * rstd, gu[v][k], bu[v][k]);
+      for (int k = 0; k < 8; ++k) x[k] = fmaf((x[k] - mean) * rstd, p[k], q[k]);
     }
+    lam.get(p);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) h[v][k] = fmaf(lam[v][k], h[v][k], a.g ? sigma(g[v][k]) * x[v][k] : x[v][k]);
+    for (int k = 0; k < 8; ++k) h[k] = fmaf(p[k], h[k], a.g ? sigma(g[k]) * x[k] : x[k]);
+    if (in && l.left > 0) {
       OpRaw<TS> o;
-      o.put(h[v]);
-      if (in && l.left[v] > 0) o.store(static_cast<TS *>(a.h) + row * a.h_ld + l.c[v], l.left[v]);
+      o.put(h);
+      o.store(static_cast<TS *>(a.h) + row * a.h_ld + l.c, l.left);
     }
     if (!a.n && !a.keep_n) continue;
     if (a.norm_n != FADE_NORM_NONE) {
       float mean, rstd;
-      row_stats<V>(rs, a.norm_n, h, l.left, l.mine, C, a.eps, mean, rstd);
+      row_stats(rs, a.norm_n, h, l.left, l.mine, C, a.eps, mean, rstd);
+      gn.get(p); bn.get(q);
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[v][k] = fmaf((h[v][k] - mean) * rstd, gn[v][k], bn[v][k]);
+      for (int k = 0; k < 8; ++k) h[k] = fmaf((h[k] - mean) * rstd, p[k], q[k]);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      OpRaw<TB> o;
-      o.put(h[v]);
-      if (a.n && in && l.left[v] > 0) o.store(static_cast<TB *>(a.n) + row * a.n_ld + l.c[v], l.left[v]);
-      o.get(h[v]);  // a checkpoint of n is one of the values as rounded
+    OpRaw<TB> o;
+    o.put(h);
+    if (a.n && in && l.left > 0) o.store(static_cast<TB *>(a.n) + row * a.n_ld + l.c, l.left);
+    if (a.keep_n) {
+      o.get(h);  // a checkpoint of n is one of the values as rounded
+      keep_row(a.keep_n, a.rows, a.width, row, in, h, l.c);
     }
-    if (a.keep_n) keep_row<V>(a.keep_n, a.rows, a.width, row, in, h, l.c);
   }
 }
 
 // ---------------------------------------------------------------------------------------------------
 // The gradient
 // ---------------------------------------------------------------------------------------------------
-// partial sums of the parameters' gradients: [workgroup][5][width rounded up to 8]
+// partial sums of the parameters' gradients: [workgroup][5][width rounded up to 8]; one value of lam: its sum at the first column
 enum { PART_GU = 0, PART_BU, PART_GN, PART_BN, PART_LAM, PARTS };
 __host__ __device__ inline size_t part_width(int width) { return (size_t)((width + 7) / 8 * 8); }
 
@@ -241,242 +240,210 @@ struct SavedKeep {  // or from its checkpoint
   __device__ __forceinline__ void get(float x[8]) const { op_keep_unpack(q, op_keep_unit(e), x); }
 };
 
-template <int L, int V, typename TS, typename TB, bool KEPT> __global__ __launch_bounds__(most(L, 256)) void join_grad_kernel(JoinArgs a) {
+template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds__(most(L, 256)) void join_grad_kernel(JoinArgs a) {
   typedef RowSums<L> Sums;
+  typedef Param<(L <= 512)> P;
   typedef std::conditional_t<KEPT, SavedKeep, SavedRaw<TS>> RawS;
   typedef std::conditional_t<KEPT, SavedKeep, SavedRaw<TB>> RawB;
   constexpr int GROUPS = Sums::GROUPS;
   __shared__ float lds[2][GROUPS][Sums::W > 0 ? Sums::W : 1][4];
-  __shared__ __align__(16) float fold[GROUPS > 1 ? 256 * 8 * V : 4];
-  const Lanes<L, V> l(a.width);
+  __shared__ __align__(16) float fold[GROUPS > 1 ? 256 * 8 : 4];
+  const Lane<L> l(a.width);
   Sums rs{lds, 0, l.group, l.lane / 64};
-  float gu[V][8], bu[V][8], gn[V][8], lam[V][8], part[PARTS][V][8];
+  const P gu(a.gamma_u, 1.0f, l.c, l.left), bu(a.beta_u, 0.0f, l.c, l.left), gn(a.gamma_n, 1.0f, l.c, l.left),
+      lam(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c, l.left);
+  float part[PARTS][8];
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    param8(a.gamma_u, 1.0f, l.c[v], l.left[v], gu[v]);
-    param8(a.beta_u, 0.0f, l.c[v], l.left[v], bu[v]);
-    param8(a.gamma_n, 1.0f, l.c[v], l.left[v], gn[v]);
-    param8(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c[v], l.left[v], lam[v]);
+  for (int k = 0; k < 8; ++k)
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) part[p][v][k] = 0.0f;
-  }
+    for (int p = 0; p < PARTS; ++p) part[p][k] = 0.0f;
   const float C = (float)a.width, inv = 1.0f / C;
   const void *src_r = KEPT ? a.keep_r : a.r, *src_u = KEPT ? a.keep_u : a.u, *src_g = KEPT ? a.keep_g : a.g;
-  for (uint32_t base = blockIdx.x * GROUPS; base < (uint32_t)a.rows; base += gridDim.x * GROUPS) {
-    const bool in = base + l.group < (uint32_t)a.rows;
+  RawS raw_r;
+  RawB raw_u, raw_g;
+  OpRaw<TS> raw_dh;
+  OpRaw<TB> raw_dn;
+  auto load = [&](size_t row) {
+    raw_r.zero(); raw_u.zero(); raw_g.zero(); raw_dh.zero(); raw_dn.zero();
+    if (row < (size_t)a.rows && l.left > 0) {
+      raw_r.load(src_r, a.r_ld, a.rows, a.width, row, l.c, l.left);
+      raw_u.load(src_u, a.u_ld, a.rows, a.width, row, l.c, l.left);
+      if (src_g) raw_g.load(src_g, a.g_ld, a.rows, a.width, row, l.c, l.left);
+      if (a.dh) raw_dh.load(static_cast<const TS *>(a.dh) + row * a.dh_ld + l.c, l.left);
+      if (a.dn) raw_dn.load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c, l.left);
+    }
+  };
+  uint32_t base = blockIdx.x * GROUPS;
+  load(base + l.group);
+  for (; base < (uint32_t)a.rows; base += gridDim.x * GROUPS) {
     const size_t row = base + l.group;
-    RawS raw_r[V];
-    RawB raw_u[V], raw_g[V];
-    OpRaw<TS> raw_dh[V];
-    OpRaw<TB> raw_dn[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      raw_r[v].zero(); raw_u[v].zero(); raw_g[v].zero(); raw_dh[v].zero(); raw_dn[v].zero();
-      if (in && l.left[v] > 0) {
-        raw_r[v].load(src_r, a.r_ld, a.rows, a.width, row, l.c[v], l.left[v]);
-        raw_u[v].load(src_u, a.u_ld, a.rows, a.width, row, l.c[v], l.left[v]);
-        if (src_g) raw_g[v].load(src_g, a.g_ld, a.rows, a.width, row, l.c[v], l.left[v]);
-        if (a.dh) raw_dh[v].load(static_cast<const TS *>(a.dh) + row * a.dh_ld + l.c[v], l.left[v]);
-        if (a.dn) raw_dn[v].load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c[v], l.left[v]);
-      }
-    }
+    const bool in = row < (size_t)a.rows;
     // forward again: uhat, z, sigma(g), h
-    float uhat[V][8], z[V][8], sg[V][8], r[V][8], t[V][8], rstd_u = 1.0f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      raw_u[v].get(uhat[v]);
-      raw_r[v].get(r[v]);
-      raw_g[v].get(sg[v]);
-      raw_dh[v].get(t[v]);
-    }
+    float uhat[8], z[8], sg[8], r[8], t[8], w[8], rstd_u = 1.0f;
+    raw_u.get(uhat); raw_r.get(r); raw_g.get(sg); raw_dh.get(t);
+    const OpRaw<TB> this_dn = raw_dn;
+    load(row + gridDim.x * GROUPS);
     if (a.norm_u != FADE_NORM_NONE) {
-      float mean;
-      row_stats<V>(rs, a.norm_u, uhat, l.left, l.mine, C, a.eps, mean, rstd_u);
+      float mean, q[8];
+      row_stats(rs, a.norm_u, uhat, l.left, l.mine, C, a.eps, mean, rstd_u);
+      gu.get(w); bu.get(q);
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          uhat[v][k] = (uhat[v][k] - mean) * rstd_u;
-          z[v][k] = fmaf(uhat[v][k], gu[v][k], bu[v][k]);
-        }
+      for (int k = 0; k < 8; ++k) {
+        uhat[k] = (uhat[k] - mean) * rstd_u;
+        z[k] = fmaf(uhat[k], w[k], q[k]);
+      }
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) z[v][k] = uhat[v][k];
+      for (int k = 0; k < 8; ++k) z[k] = uhat[k];
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sg[v][k] = src_g ? sigma(sg[v][k]) : 1.0f;
+    for (int k = 0; k < 8; ++k) sg[k] = src_g ? sigma(sg[k]) : 1.0f;
     // t = dh + N_n'(dn)
     if (a.dn) {
+      float e[8];
+      this_dn.get(e);
       if (a.norm_n != FADE_NORM_NONE) {
-        float h[V][8], mean, rstd, s[2] = {0.0f, 0.0f};
+        float h[8], mean, rstd, s[2] = {0.0f, 0.0f};
+        lam.get(w);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int k = 0; k < 8; ++k) h[k] = fmaf(w[k], r[k], sg[k] * z[k]);
+        row_stats(rs, a.norm_n, h, l.left, l.mine, C, a.eps, mean, rstd);
+        gn.get(w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) h[v][k] = fmaf(lam[v][k], r[v][k], sg[v][k] * z[v][k]);
-        row_stats<V>(rs, a.norm_n, h, l.left, l.mine, C, a.eps, mean, rstd);
-        float e[V][8];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          raw_dn[v].get(e[v]);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            h[v][k] = (h[v][k] - mean) * rstd;
-            part[PART_GN][v][k] = fmaf(e[v][k], h[v][k], part[PART_GN][v][k]);
-            part[PART_BN][v][k] += e[v][k];
-            e[v][k] *= gn[v][k];
-            s[0] += e[v][k];
-            s[1] = fmaf(e[v][k], h[v][k], s[1]);
-          }
+        for (int k = 0; k < 8; ++k) {
+          h[k] = (h[k] - mean) * rstd;
+          part[PART_GN][k] = fmaf(e[k], h[k], part[PART_GN][k]);
+          part[PART_BN][k] += e[k];
+          e[k] *= w[k];
+          s[0] += e[k];
+          s[1] = fmaf(e[k], h[k], s[1]);
         }
         rs.sum(s);
         const float level = a.norm_n == FADE_NORM_LAYER ? s[0] * inv : 0.0f, along = s[1] * inv;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) t[v][k] = fmaf(rstd, fmaf(-h[v][k], along, e[v][k] - level), t[v][k]);
+        for (int k = 0; k < 8; ++k) t[k] = fmaf(rstd, fmaf(-h[k], along, e[k] - level), t[k]);
       } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float e[8];
-          raw_dn[v].get(e);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) t[v][k] += e[k];
-        }
+        for (int k = 0; k < 8; ++k) t[k] += e[k];
       }
     }
     // through the join
+    lam.get(w);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float x[8];
+    for (int k = 0; k < 8; ++k) {
+      part[PART_LAM][k] = fmaf(t[k], r[k], part[PART_LAM][k]);
+      r[k] = w[k] * t[k];
+    }
+    const bool store = in && l.left > 0;
+    if (a.dr && store) {
+      OpRaw<TS> o;
+      o.put(r);
+      o.store(static_cast<TS *>(a.dr) + row * a.dr_ld + l.c, l.left);
+    }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        part[PART_LAM][v][k] = fmaf(t[v][k], r[v][k], part[PART_LAM][v][k]);
-        x[k] = lam[v][k] * t[v][k];
-      }
-      if (a.dr && in && l.left[v] > 0) {
-        OpRaw<TS> o;
-        o.put(x);
-        o.store(static_cast<TS *>(a.dr) + row * a.dr_ld + l.c[v], l.left[v]);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float dz = t[v][k] * sg[v][k];
-        x[k] = dz * z[v][k] * (1.0f - sg[v][k]);
-        t[v][k] = dz;
-      }
-      if (a.dg && in && l.left[v] > 0) {
-        OpRaw<TB> o;
-        o.put(x);
-        o.store(static_cast<TB *>(a.dg) + row * a.dg_ld + l.c[v], l.left[v]);
-      }
+    for (int k = 0; k < 8; ++k) {
+      t[k] *= sg[k];
+      sg[k] = t[k] * z[k] * (1.0f - sg[k]);
+    }
+    if (a.dg && store) {
+      OpRaw<TB> o;
+      o.put(sg);
+      o.store(static_cast<TB *>(a.dg) + row * a.dg_ld + l.c, l.left);
     }
     // du = N_u'(dz)
     if (a.norm_u != FADE_NORM_NONE) {
       float s[2] = {0.0f, 0.0f};
+      gu.get(w);
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          part[PART_GU][v][k] = fmaf(t[v][k], uhat[v][k], part[PART_GU][v][k]);
-          part[PART_BU][v][k] += t[v][k];
-          t[v][k] *= gu[v][k];
-          s[0] += t[v][k];
-          s[1] = fmaf(t[v][k], uhat[v][k], s[1]);
-        }
+      for (int k = 0; k < 8; ++k) {
+        part[PART_GU][k] = fmaf(t[k], uhat[k], part[PART_GU][k]);
+        part[PART_BU][k] += t[k];
+        t[k] *= w[k];
+        s[0] += t[k];
+        s[1] = fmaf(t[k], uhat[k], s[1]);
+      }
       rs.sum(s);
       const float level = a.norm_u == FADE_NORM_LAYER ? s[0] * inv : 0.0f, along = s[1] * inv;
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[v][k] = rstd_u * fmaf(-uhat[v][k], along, t[v][k] - level);
+      for (int k = 0; k < 8; ++k) t[k] = rstd_u * fmaf(-uhat[k], along, t[k] - level);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (a.du && in && l.left[v] > 0) {
-        OpRaw<TB> o;
-        o.put(t[v]);
-        o.store(static_cast<TB *>(a.du) + row * a.du_ld + l.c[v], l.left[v]);
-      }
+    if (a.du && store) {
+      OpRaw<TB> o;
+      o.put(t);
+      o.store(static_cast<TB *>(a.du) + row * a.du_ld + l.c, l.left);
+    }
   }
   // the workgroup's sums over its rows, its groups' in order
+  if (a.lam_count == 1) {
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[0] += part[PART_LAM][k];
+    rs.sum(s);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) part[PART_LAM][k] = s[0];
+  }
   float *dst = a.work + (size_t)blockIdx.x * PARTS * part_width(a.width);
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) {
     if constexpr (GROUPS > 1) {
       __syncthreads();
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) fold[((v * GROUPS + l.group) * 8 + k) * L + l.lane] = part[p][v][k];
+      for (int k = 0; k < 8; ++k) fold[(l.group * 8 + k) * L + l.lane] = part[p][k];
       __syncthreads();
       if (l.group == 0)
         for (int g = 1; g < GROUPS; ++g)
 #pragma unroll
-          for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) part[p][v][k] += fold[((v * GROUPS + g) * 8 + k) * L + l.lane];
+          for (int k = 0; k < 8; ++k) part[p][k] += fold[(g * 8 + k) * L + l.lane];
     }
-    if (l.group == 0)
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (l.left[v] > 0) {
-          OpRaw<float> o;
-          o.put(part[p][v]);
-          o.store(dst + p * part_width(a.width) + l.c[v], 8);
-        }
+    if (l.group == 0 && l.left > 0) {
+      OpRaw<float> o;
+      o.put(part[p]);
+      o.store(dst + p * part_width(a.width) + l.c, 8);
+    }
   }
 }
 
-// The workgroups' partial sums, in order: 16 slices of them side by side per column, then the slices.
-// One value of lam: its column sums are added up as well, by the one workgroup that has them all.
+// The workgroups' partial sums, in order: 64 columns of one parameter a workgroup, four a lane, 64 slices of the partial sums side by side, then the slices in four
+// ranges.
 __global__ __launch_bounds__(1024) void join_finish_kernel(JoinArgs a, int blocks) {
-  __shared__ float sums[16][65];
-  const int p = blockIdx.y;
+  __shared__ float sums[64][68], four[4][64];
+  const int p = blockIdx.y, width = p == PART_LAM && a.lam_count == 1 ? 1 : a.width;
   float *dst = p == PART_GU ? a.d_gamma_u : p == PART_BU ? a.d_beta_u : p == PART_GN ? a.d_gamma_n : p == PART_BN ? a.d_beta_n : a.d_lam;
-  if (!dst) return;
-  const bool one = p == PART_LAM && a.lam_count == 1;
-  if (one && blockIdx.x > 0) return;
-  const int slice = threadIdx.x >> 6, lane = threadIdx.x & 63, per = (blocks + 15) / 16;
+  const int c0 = blockIdx.x * 64, slice = threadIdx.x >> 4, quad = (threadIdx.x & 15) * 4, per = (blocks + 63) / 64;
+  if (!dst || c0 >= width) return;
   const size_t w = part_width(a.width);
-  float total = 0.0f;
-  for (int c0 = blockIdx.x * 64; c0 < a.width; c0 += one ? 64 : a.width) {
-    float s = 0.0f;
-    const int c = c0 + lane;
-    if (c < a.width)
-      for (int b = slice * per; b < (slice + 1) * per && b < blocks; ++b) s += a.work[((size_t)b * PARTS + p) * w + c];
-    __syncthreads();
-    sums[slice][lane] = s;
-    __syncthreads();
-    if (slice == 0) {
-      s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s += sums[i][lane];
-      if (one) total += s;
-      else if (c < a.width) dst[c] = a.accumulate ? dst[c] + s : s;
-    }
+  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c0 + quad < (int)w) {
+    const float *src = a.work + p * w + c0 + quad;
+    const int end = (slice + 1) * per < blocks ? (slice + 1) * per : blocks;
+#pragma unroll 8
+    for (int b = slice * per; b < end; ++b) s += *reinterpret_cast<const f32x4 *>(src + (size_t)b * PARTS * w);
   }
-  if (one && slice == 0) {
-    total = fade_lanes_sum(total);
-    if (lane == 0) dst[0] = a.accumulate ? dst[0] + total : total;
+  *reinterpret_cast<f32x4 *>(&sums[slice][quad]) = s;
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += sums[threadIdx.x / 64 * 16 + i][threadIdx.x & 63];
+    four[threadIdx.x >> 6][threadIdx.x & 63] = v;
+  }
+  __syncthreads();
+  const int c = c0 + threadIdx.x;
+  if (threadIdx.x < 64 && c < width) {
+    const float v = ((four[0][threadIdx.x] + four[1][threadIdx.x]) + four[2][threadIdx.x]) + four[3][threadIdx.x];
+    dst[c] = a.accumulate ? dst[c] + v : v;
   }
 }
 
-template <typename F> hipError_t with_shape(const JoinShape &sh, F &&f) {
-  if (sh.V == 2) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
-  else switch (sh.L) {
-    case 16: f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}); break;
-    case 32: f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{}); break;
-    case 64: f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{}); break;
-    case 128: f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{}); break;
-    case 256: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{}); break;
-    case 512: f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{}); break;
-    default: f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{}); break;
+template <typename F> hipError_t with_lanes(int lanes, F &&f) {
+  switch (lanes) {
+    case 16: f(std::integral_constant<int, 16>{}); break;
+    case 32: f(std::integral_constant<int, 32>{}); break;
+    case 64: f(std::integral_constant<int, 64>{}); break;
+    case 128: f(std::integral_constant<int, 128>{}); break;
+    case 256: f(std::integral_constant<int, 256>{}); break;
+    case 512: f(std::integral_constant<int, 512>{}); break;
+    default: f(std::integral_constant<int, 1024>{}); break;
   }
   return hipGetLastError();
 }
@@ -493,9 +460,9 @@ hipError_t fade_join_launch(const JoinArgs &a, hipStream_t s) {
   const JoinShape sh = join_shape(a.width);
   const int need = (a.rows + sh.groups - 1) / sh.groups, blocks = need < 2048 ? need : 2048;
   return with_types(a, [&](auto st, auto br) {
-    return with_shape(sh, [&](auto l, auto v) {
-      constexpr int L = decltype(l)::value, V = decltype(v)::value;
-      hipLaunchKernelGGL((join_kernel<L, V, decltype(st), decltype(br)>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
+    return with_lanes(sh.lanes, [&](auto l) {
+      constexpr int L = decltype(l)::value;
+      hipLaunchKernelGGL((join_kernel<L, decltype(st), decltype(br)>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
     });
   });
 }
@@ -508,12 +475,12 @@ hipError_t fade_join_grad_launch(const JoinArgs &a, hipStream_t s) {
   const int blocks = grad_blocks(a.rows, a.width);
   if (blocks) {
     const hipError_t e = with_types(a, [&](auto st, auto br) {
-      return with_shape(sh, [&](auto l, auto v) {
-        constexpr int L = decltype(l)::value, V = decltype(v)::value;
+      return with_lanes(sh.lanes, [&](auto l) {
+        constexpr int L = decltype(l)::value;
         typedef decltype(st) TS;
         typedef decltype(br) TB;
-        if (a.kept) hipLaunchKernelGGL((join_grad_kernel<L, V, TS, TB, true>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
-        else hipLaunchKernelGGL((join_grad_kernel<L, V, TS, TB, false>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
+        if (a.kept) hipLaunchKernelGGL((join_grad_kernel<L, TS, TB, true>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
+        else hipLaunchKernelGGL((join_grad_kernel<L, TS, TB, false>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
       });
     });
     if (e != hipSuccess) return e;

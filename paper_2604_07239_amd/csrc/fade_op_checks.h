@@ -9,7 +9,7 @@
 
 namespace fade_op {
 
-constexpr size_t ROWS = 0x7fffffff, WIDTH = (size_t)1 << 20, VOCAB = (size_t)1 << 20, GRAD_WIDTH = 65536, GRAD_LD = (size_t)1 << 22, JOIN_WIDTH = 16384;
+constexpr size_t ROWS = 0x7fffffff, WIDTH = (size_t)1 << 20, VOCAB = (size_t)1 << 20, GRAD_WIDTH = 65536, GRAD_LD = (size_t)1 << 22, JOIN_WIDTH = 8192;
 
 inline bool type(uint32_t t) { return t == FADE_F32 || t == FADE_BF16; }
 inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }

@@ -88,18 +88,18 @@ inline WgradPlan wgrad_plan(size_t rows, size_t K, size_t N, bool f32) {
   return best;
 }
 
-// Lanes for a row: 8 columns each, from 16 to a workgroup of 1024; two steps of 8 columns above 8192.
+// Lanes for a row of the join, 8 columns each, and the rows a workgroup has at a time.
 struct JoinShape {
-  int L, V, groups;
+  int lanes, groups;
 };
 inline JoinShape join_shape(size_t width) {
-  int L = 16;
-  while (L < 1024 && (size_t)L * 8 < width) L *= 2;
-  return {L, (size_t)L * 8 < width ? 2 : 1, L >= 256 ? 1 : 256 / L};
+  int lanes = 16;
+  while ((size_t)lanes * 8 < width) lanes *= 2;
+  return {lanes, lanes >= 256 ? 1 : 256 / lanes};
 }
 inline int grad_blocks(size_t rows, size_t width) {
   const JoinShape sh = join_shape(width);
-  const size_t need = (rows + sh.groups - 1) / sh.groups, most = sh.L >= 512 ? 256 : 512;
+  const size_t need = (rows + sh.groups - 1) / sh.groups, most = sh.lanes >= 512 ? 256 : 512;
   return (int)(need < most ? need : most);
 }
 

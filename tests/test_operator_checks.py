@@ -101,7 +101,7 @@ int main() {
   NO(join(NULL));
   NO(with([](A a) { a.struct_size--; }));
   NO(with([](A a) { a.width = 0; }));
-  NO(with([](A a) { a.width = 16385; }));
+  NO(with([](A a) { a.width = 8193; }));
   NO(with([](A a) { a.rows = (size_t)1 << 31; }));
   NO(with([](A a) { a.norm_u = 3; }));
   NO(with([](A a) { a.norm_n = 3; }));
@@ -199,9 +199,9 @@ int main() {
           WANT((long long)p.ranges * p.per >= p.units);
           WANT(p.units == 0 || (long long)(p.ranges - 1) * p.per < p.units);  // no range is empty
         }
-  for (size_t width = 1; width <= 16384; width += width < 300 ? 1 : 97) {
+  for (size_t width = 1; width <= 8192; width += width < 300 ? 1 : 97) {
     const JoinShape s = join_shape(width);
-    WANT((size_t)s.L * s.V * 8 >= width && s.L >= 16 && s.L <= 1024 && s.groups >= 1);
+    WANT((size_t)s.lanes * 8 >= width && s.lanes >= 16 && s.lanes <= 1024 && s.groups >= 1);
     for (size_t rows : {(size_t)0, (size_t)1, (size_t)100, (size_t)0x7fffffff}) {
       const int b = grad_blocks(rows, width);
       WANT(b >= 0 && b <= 1024 && (rows == 0 || b >= 1) && (size_t)b * s.groups < rows + s.groups);
@@ -223,7 +223,7 @@ def test_arguments_and_sizes_as_the_library_sees_them():
     assert L.fade_checkpoint_nbytes(3, 33) == 3 * 2 * 33
     assert L.fade_checkpoint_nbytes(0, 33) == 0 and L.fade_checkpoint_nbytes(3, 0) == 0 and L.fade_checkpoint_nbytes(3, (1 << 20) + 1) == 0
     assert L.fade_embed_grad_work(1 << 31, 10, 8) == 0 and L.fade_embed_grad_work(5, 0, 8) == 0 and L.fade_embed_grad_work(0, 10, 8) > 0
-    assert L.fade_join_grad_work(5, 16385) == 0 and L.fade_join_grad_work(0, 8) > 0
+    assert L.fade_join_grad_work(5, 8193) == 0 and L.fade_join_grad_work(0, 8) > 0
     assert L.fade_checkpoint_weight_grad_work(5, 65537, 8) == 0 and L.fade_checkpoint_weight_grad_work(0, 8, 8) >= 16
     # without a context nothing else is looked at
     assert L.fade_embed(None, None, 0, 0, None, 0, 0, 0, 0, 1.0, None, 0, 0) == -1
