@@ -6,6 +6,8 @@
 // LayerNorm's variance is the mean of the squares of centred values: the difference of E[x^2] and mean^2 loses what a large mean covers.
 // Parameter gradients are sums over the rows: a workgroup keeps its columns' sums in registers over all its rows and leaves one partial sum per column,
 // which a second kernel adds in order. No atomics.
+#include <type_traits>
+
 #include "../../include/fade.h"
 #include "fade_op_rules.h"
 #include "fade_ops.h"
@@ -15,49 +17,78 @@ using namespace fade_op;
 
 constexpr int most(int a, int b) { return a > b ? a : b; }
 
+// Sum over the L lanes of a row in this wavefront: 64 lanes by shifts inside the rows of 16 and broadcasts of their last lanes (one add each) into lane 63,
+// fewer lanes by a butterfly.
+template <int L> __device__ __forceinline__ float wave_total(float v) {
+  if constexpr (L < 64) return fade_lanes_sum<L>(v);
+  auto add = [&](auto ctrl, auto rows) { v += __builtin_bit_cast(float, fade_dpp<decltype(ctrl)::value, decltype(rows)::value>(fade_bits(v))); };
+  typedef std::integral_constant<int, 0xf> All;
+  add(std::integral_constant<int, 0x111>{}, All{});
+  add(std::integral_constant<int, 0x112>{}, All{});
+  add(std::integral_constant<int, 0x114>{}, All{});
+  add(std::integral_constant<int, 0x118>{}, All{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)fade_bits(v), 63));
+}
+// s / n from a reciprocal good to an ulp: the remainder's quotient makes up for it (a row of equal values has exactly that mean)
+__device__ __forceinline__ float quotient(float s, float n, float inv) {
+  const float q = s * inv;
+  return fmaf(fmaf(-n, q, s), inv, q);
+}
 // Sums over the L lanes of a row, the same value in each of them. Above a wavefront through LDS: one barrier a sum, in two places in turn
 // (a wavefront may be one sum ahead of another, never two).
 template <int L> struct RowSums {
-  static constexpr int W = L / 64, GROUPS = L >= 256 ? 1 : 256 / L;  // wavefronts of a row; rows of a workgroup
-  float (*lds)[GROUPS][W > 0 ? W : 1][4];                            // [2]
-  int place = 0, group, wave;
+  static constexpr int W = L >= 64 ? L / 64 : 1, GROUPS = L >= 256 ? 1 : 256 / L;  // wavefronts of a row; rows of a workgroup
+  typedef float Lds[2][GROUPS][2][W < 4 ? 4 : W];
+  Lds &lds;
+  int group, wave, width, place = 0;
   template <int N> __device__ __forceinline__ void sum(float (&v)[N]) {
+    static_assert(N <= 2, "places");
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = fade_lanes_sum<(L < 64 ? L : 64)>(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = wave_total<L>(v[i]);
     if constexpr (W > 1) {
       if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int i = 0; i < N; ++i) lds[place][group][wave][i] = v[i];
+        for (int i = 0; i < N; ++i) lds[place][group][i][wave] = v[i];
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        v[i] = 0.0f;
+        v[i] = lds[place][group][i][0];
 #pragma unroll
-        for (int w = 0; w < W; ++w) v[i] += lds[place][group][w][i];
+        for (int w = 1; w < W; ++w) v[i] += lds[place][group][i][w];
       }
       place ^= 1;
     }
   }
-  // mean and sum of squared distances from it, of `mine` values in this wavefront and C in the row: centred on the wavefront's mean, then moved to the row's
-  template <typename F> __device__ __forceinline__ void moments(float s, float mine, float C, float &mean, float &sq, F &&centred) {
-    s = fade_lanes_sum<(L < 64 ? L : 64)>(s);
-    mean = mine > 0.0f ? s / mine : 0.0f;
-    sq = fade_lanes_sum<(L < 64 ? L : 64)>(centred(mean));
+  __device__ __forceinline__ float columns(int w) const {  // of the row's w-th wavefront
+    const int have = width - w * 512, span = (L < 64 ? L : 64) * 8;
+    return (float)(have < 0 ? 0 : have > span ? span : have);
+  }
+  // mean and sum of squared distances from it: centred on the wavefront's own mean, then moved to the row's
+  template <typename F> __device__ __forceinline__ void moments(float s, float inv, float &mean, float &sq, F &&centred) {
+    s = wave_total<L>(s);
+    const float mine = W > 1 ? fmaxf(columns(wave), 1.0f) : (float)width;
+    mean = quotient(s, mine, W > 1 ? __builtin_amdgcn_rcpf(mine) : inv);
+    sq = wave_total<L>(centred(mean));
     if constexpr (W > 1) {
       if ((threadIdx.x & 63) == 0) {
-        float *p = lds[place][group][wave];
-        p[0] = mean; p[1] = sq; p[2] = mine; p[3] = s;
+        lds[place][group][0][wave] = mean;
+        lds[place][group][1][wave] = sq;
       }
       __syncthreads();
-      float all = 0.0f;
+      float all = 0.0f, m[W];
 #pragma unroll
-      for (int w = 0; w < W; ++w) all += lds[place][group][w][3];
-      mean = all / C;
+      for (int w = 0; w < W; ++w) {
+        m[w] = lds[place][group][0][w];
+        all = fmaf(m[w], columns(w), all);
+      }
+      mean = quotient(all, (float)width, inv);
       sq = 0.0f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float d = lds[place][group][w][0] - mean;
-        sq += fmaf(lds[place][group][w][2] * d, d, lds[place][group][w][1]);
+        const float d = m[w] - mean;
+        sq += fmaf(d * d, columns(w), lds[place][group][1][w]);
       }
       place ^= 1;
     }
@@ -65,22 +96,27 @@ template <int L> struct RowSums {
 };
 
 // statistics of a row's values x: mean (0 unless LayerNorm) and 1 / sigma
-template <int L>
-__device__ __forceinline__ void row_stats(RowSums<L> &rs, int norm, const float (&x)[8], int left, float mine, float C, float eps, float &mean, float &rstd) {
+template <int L, bool WHOLE>
+__device__ __forceinline__ void row_stats(RowSums<L> &rs, int norm, const float (&x)[8], int left, float inv, float eps, float &mean, float &rstd) {
   float sq;
   if (norm == FADE_NORM_LAYER) {
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) s += x[k];  // columns that do not exist hold zeros
-    rs.moments(s, mine, C, mean, sq, [&](float m) {
+    rs.moments(s, inv, mean, sq, [&](float m) {
       float q = 0.0f;
-      if (left >= 8) {
+      if (WHOLE || left >= 8 || left <= 0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) q = fmaf(x[k] - m, x[k] - m, q);
-      } else {
+        for (int k = 0; k < 8; ++k) {
+          const float d = x[k] - m;
+          q = fmaf(d, d, q);
+        }
+        return left > 0 ? q : 0.0f;
+      }
 #pragma unroll
-        for (int k = 0; k < 7; ++k)
-          if (k < left) q = fmaf(x[k] - m, x[k] - m, q);
+      for (int k = 0; k < 7; ++k) {
+        const float d = x[k] - m;
+        if (k < left) q = fmaf(d, d, q);
       }
       return q;
     });
@@ -92,7 +128,7 @@ __device__ __forceinline__ void row_stats(RowSums<L> &rs, int norm, const float 
     mean = 0.0f;
     sq = q[0];
   }
-  rstd = 1.0f / sqrtf(sq / C + eps);
+  rstd = __builtin_amdgcn_rsqf(fmaf(sq, inv, eps));  // good to an ulp
 }
 
 // 8 columns of a parameter; `otherwise` where there is none, zeros past the row's end
@@ -127,18 +163,18 @@ template <bool HELD> struct Param {
 // sigma(x) = 1 / (1 + exp(-x)); fade_sigmoid's reciprocal is the hardware's, good to an ulp
 __device__ __forceinline__ float sigma(float x) { return fade_sigmoid(x); }
 
-template <int L> struct Lane {
+template <int L> struct Lane {  // the same row for a whole wavefront is known to be one: addresses of rows are scalar then
   int group, lane, c, left;
-  float mine;  // columns of this wavefront (of this row where a wavefront holds several)
   __device__ __forceinline__ Lane(int width) {
-    group = threadIdx.x / L;
+    group = L >= 256 ? 0 : L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L;
     lane = threadIdx.x % L;
     c = lane * 8;
     left = width - c;
-    const int have = width - (L > 64 ? lane / 64 * 512 : 0), span = (L < 64 ? L : 64) * 8;
-    mine = (float)(have < 0 ? 0 : have > span ? span : have);
   }
+  __device__ __forceinline__ int wave() const { return L > 64 ? __builtin_amdgcn_readfirstlane(lane / 64) : 0; }
 };
+// how many of 8 columns to move: all of them on rows of whole pieces
+template <bool WHOLE> __device__ __forceinline__ int op_left(int left) { return WHOLE ? 8 : left; }
 
 __device__ __forceinline__ void keep_row(uint8_t *keep, int rows, int width, size_t row, bool in, const float (&x)[8], int c) {
   const int groups = (width + 31) / 32;
@@ -151,30 +187,33 @@ __device__ __forceinline__ void keep_row(uint8_t *keep, int rows, int width, siz
 }
 
 // A workgroup takes rows in strides of the grid; the next rows' operands are on their way while it works on these.
-template <int L, typename TS, typename TB> __global__ __launch_bounds__(most(L, 256)) void join_kernel(JoinArgs a) {
+// WHOLE: the width is a multiple of 8.
+template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bounds__(most(L, 256)) void join_kernel(JoinArgs a) {
   typedef RowSums<L> Sums;
   typedef Param<(L <= 512)> P;
-  __shared__ float lds[2][Sums::GROUPS][Sums::W > 0 ? Sums::W : 1][4];
+  __shared__ __align__(16) typename Sums::Lds lds;
   const Lane<L> l(a.width);
-  Sums rs{lds, 0, l.group, l.lane / 64};
+  Sums rs{lds, l.group, l.wave(), a.width};
   const P gu(a.gamma_u, 1.0f, l.c, l.left), bu(a.beta_u, 0.0f, l.c, l.left), gn(a.gamma_n, 1.0f, l.c, l.left), bn(a.beta_n, 0.0f, l.c, l.left),
       lam(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c, l.left);
-  const float C = (float)a.width;
+  const float inv = 1.0f / (float)a.width;
   OpRaw<TS> raw_r;
   OpRaw<TB> raw_u, raw_g;
-  auto load = [&](size_t row) {
-    raw_r.zero(); raw_u.zero(); raw_g.zero();
-    if (row < (size_t)a.rows && l.left > 0) {
-      raw_r.load(static_cast<const TS *>(a.r) + row * a.r_ld + l.c, l.left);
-      raw_u.load(static_cast<const TB *>(a.u) + row * a.u_ld + l.c, l.left);
-      if (a.g) raw_g.load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c, l.left);
+  raw_r.zero(); raw_u.zero(); raw_g.zero();  // and so they stay in lanes past the row's end
+  auto load = [&](size_t row) {              // past the last row: that one again
+    if (row >= (size_t)a.rows) row = a.rows - 1;
+    if (l.left > 0) {
+      const int left = op_left<WHOLE>(l.left);
+      raw_r.load(static_cast<const TS *>(a.r) + row * a.r_ld + l.c, left);
+      raw_u.load(static_cast<const TB *>(a.u) + row * a.u_ld + l.c, left);
+      if (a.g) raw_g.load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c, left);
     }
   };
   uint32_t base = blockIdx.x * Sums::GROUPS;
   load(base + l.group);
   for (; base < (uint32_t)a.rows; base += gridDim.x * Sums::GROUPS) {
     const size_t row = base + l.group;
-    const bool in = row < (size_t)a.rows;  // the workgroup's barriers are for all its rows
+    const bool in = Sums::GROUPS == 1 || row < (size_t)a.rows;  // the workgroup's barriers are for all its rows
     float x[8], h[8], g[8], p[8], q[8];
     raw_u.get(x); raw_r.get(h); raw_g.get(g);
     load(row + gridDim.x * Sums::GROUPS);
@@ -183,7 +222,7 @@ template <int L, typename TS, typename TB> __global__ __launch_bounds__(most(L, 
     if (a.keep_g) keep_row(a.keep_g, a.rows, a.width, row, in, g, l.c);
     if (a.norm_u != FADE_NORM_NONE) {
       float mean, rstd;
-      row_stats(rs, a.norm_u, x, l.left, l.mine, C, a.eps, mean, rstd);
+      row_stats<L, WHOLE>(rs, a.norm_u, x, l.left, inv, a.eps, mean, rstd);
       gu.get(p); bu.get(q);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = fmaf((x[k] - mean) * rstd, p[k], q[k]);
@@ -194,19 +233,19 @@ template <int L, typename TS, typename TB> __global__ __launch_bounds__(most(L, 
     if (in && l.left > 0) {
       OpRaw<TS> o;
       o.put(h);
-      o.store(static_cast<TS *>(a.h) + row * a.h_ld + l.c, l.left);
+      o.store(static_cast<TS *>(a.h) + row * a.h_ld + l.c, op_left<WHOLE>(l.left));
     }
     if (!a.n && !a.keep_n) continue;
     if (a.norm_n != FADE_NORM_NONE) {
       float mean, rstd;
-      row_stats(rs, a.norm_n, h, l.left, l.mine, C, a.eps, mean, rstd);
+      row_stats<L, WHOLE>(rs, a.norm_n, h, l.left, inv, a.eps, mean, rstd);
       gn.get(p); bn.get(q);
 #pragma unroll
       for (int k = 0; k < 8; ++k) h[k] = fmaf((h[k] - mean) * rstd, p[k], q[k]);
     }
     OpRaw<TB> o;
     o.put(h);
-    if (a.n && in && l.left > 0) o.store(static_cast<TB *>(a.n) + row * a.n_ld + l.c, l.left);
+    if (a.n && in && l.left > 0) o.store(static_cast<TB *>(a.n) + row * a.n_ld + l.c, op_left<WHOLE>(l.left));
     if (a.keep_n) {
       o.get(h);  // a checkpoint of n is one of the values as rounded
       keep_row(a.keep_n, a.rows, a.width, row, in, h, l.c);
@@ -240,16 +279,16 @@ struct SavedKeep {  // or from its checkpoint
   __device__ __forceinline__ void get(float x[8]) const { op_keep_unpack(q, op_keep_unit(e), x); }
 };
 
-template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds__(most(L, 256)) void join_grad_kernel(JoinArgs a) {
+template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __launch_bounds__(most(L, 256)) void join_grad_kernel(JoinArgs a) {
   typedef RowSums<L> Sums;
   typedef Param<(L <= 512)> P;
   typedef std::conditional_t<KEPT, SavedKeep, SavedRaw<TS>> RawS;
   typedef std::conditional_t<KEPT, SavedKeep, SavedRaw<TB>> RawB;
   constexpr int GROUPS = Sums::GROUPS;
-  __shared__ float lds[2][GROUPS][Sums::W > 0 ? Sums::W : 1][4];
+  __shared__ __align__(16) typename Sums::Lds lds;
   __shared__ __align__(16) float fold[GROUPS > 1 ? 256 * 8 : 4];
   const Lane<L> l(a.width);
-  Sums rs{lds, 0, l.group, l.lane / 64};
+  Sums rs{lds, l.group, l.wave(), a.width};
   const P gu(a.gamma_u, 1.0f, l.c, l.left), bu(a.beta_u, 0.0f, l.c, l.left), gn(a.gamma_n, 1.0f, l.c, l.left),
       lam(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c, l.left);
   float part[PARTS][8];
@@ -257,27 +296,31 @@ template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds
   for (int k = 0; k < 8; ++k)
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) part[p][k] = 0.0f;
-  const float C = (float)a.width, inv = 1.0f / C;
+  const float inv = 1.0f / (float)a.width;
   const void *src_r = KEPT ? a.keep_r : a.r, *src_u = KEPT ? a.keep_u : a.u, *src_g = KEPT ? a.keep_g : a.g;
   RawS raw_r;
   RawB raw_u, raw_g;
   OpRaw<TS> raw_dh;
   OpRaw<TB> raw_dn;
-  auto load = [&](size_t row) {
-    raw_r.zero(); raw_u.zero(); raw_g.zero(); raw_dh.zero(); raw_dn.zero();
-    if (row < (size_t)a.rows && l.left > 0) {
-      raw_r.load(src_r, a.r_ld, a.rows, a.width, row, l.c, l.left);
-      raw_u.load(src_u, a.u_ld, a.rows, a.width, row, l.c, l.left);
-      if (src_g) raw_g.load(src_g, a.g_ld, a.rows, a.width, row, l.c, l.left);
-      if (a.dh) raw_dh.load(static_cast<const TS *>(a.dh) + row * a.dh_ld + l.c, l.left);
-      if (a.dn) raw_dn.load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c, l.left);
+  auto none = [&] { raw_r.zero(); raw_u.zero(); raw_g.zero(); raw_dh.zero(); raw_dn.zero(); };
+  none();  // and so they stay in lanes past the row's end
+  auto load = [&](size_t row) {  // past the last row: that one again
+    if (row >= (size_t)a.rows) row = a.rows - 1;
+    if (l.left > 0) {
+      const int left = op_left<WHOLE>(l.left);
+      raw_r.load(src_r, a.r_ld, a.rows, a.width, row, l.c, left);
+      raw_u.load(src_u, a.u_ld, a.rows, a.width, row, l.c, left);
+      if (src_g) raw_g.load(src_g, a.g_ld, a.rows, a.width, row, l.c, left);
+      if (a.dh) raw_dh.load(static_cast<const TS *>(a.dh) + row * a.dh_ld + l.c, left);
+      if (a.dn) raw_dn.load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c, left);
     }
   };
   uint32_t base = blockIdx.x * GROUPS;
   load(base + l.group);
   for (; base < (uint32_t)a.rows; base += gridDim.x * GROUPS) {
     const size_t row = base + l.group;
-    const bool in = row < (size_t)a.rows;
+    const bool in = GROUPS == 1 || row < (size_t)a.rows;
+    if (!in) none();  // a row that is not there adds zeros
     // forward again: uhat, z, sigma(g), h
     float uhat[8], z[8], sg[8], r[8], t[8], w[8], rstd_u = 1.0f;
     raw_u.get(uhat); raw_r.get(r); raw_g.get(sg); raw_dh.get(t);
@@ -285,7 +328,7 @@ template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds
     load(row + gridDim.x * GROUPS);
     if (a.norm_u != FADE_NORM_NONE) {
       float mean, q[8];
-      row_stats(rs, a.norm_u, uhat, l.left, l.mine, C, a.eps, mean, rstd_u);
+      row_stats<L, WHOLE>(rs, a.norm_u, uhat, l.left, inv, a.eps, mean, rstd_u);
       gu.get(w); bu.get(q);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -307,7 +350,7 @@ template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds
         lam.get(w);
 #pragma unroll
         for (int k = 0; k < 8; ++k) h[k] = fmaf(w[k], r[k], sg[k] * z[k]);
-        row_stats(rs, a.norm_n, h, l.left, l.mine, C, a.eps, mean, rstd);
+        row_stats<L, WHOLE>(rs, a.norm_n, h, l.left, inv, a.eps, mean, rstd);
         gn.get(w);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -338,7 +381,7 @@ template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds
     if (a.dr && store) {
       OpRaw<TS> o;
       o.put(r);
-      o.store(static_cast<TS *>(a.dr) + row * a.dr_ld + l.c, l.left);
+      o.store(static_cast<TS *>(a.dr) + row * a.dr_ld + l.c, op_left<WHOLE>(l.left));
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -348,7 +391,7 @@ template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds
     if (a.dg && store) {
       OpRaw<TB> o;
       o.put(sg);
-      o.store(static_cast<TB *>(a.dg) + row * a.dg_ld + l.c, l.left);
+      o.store(static_cast<TB *>(a.dg) + row * a.dg_ld + l.c, op_left<WHOLE>(l.left));
     }
     // du = N_u'(dz)
     if (a.norm_u != FADE_NORM_NONE) {
@@ -370,7 +413,7 @@ template <int L, typename TS, typename TB, bool KEPT> __global__ __launch_bounds
     if (a.du && store) {
       OpRaw<TB> o;
       o.put(t);
-      o.store(static_cast<TB *>(a.du) + row * a.du_ld + l.c, l.left);
+      o.store(static_cast<TB *>(a.du) + row * a.du_ld + l.c, op_left<WHOLE>(l.left));
     }
   }
   // the workgroup's sums over its rows, its groups' in order
@@ -462,7 +505,8 @@ hipError_t fade_join_launch(const JoinArgs &a, hipStream_t s) {
   return with_types(a, [&](auto st, auto br) {
     return with_lanes(sh.lanes, [&](auto l) {
       constexpr int L = decltype(l)::value;
-      hipLaunchKernelGGL((join_kernel<L, decltype(st), decltype(br)>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
+      if (a.width % 8 == 0) hipLaunchKernelGGL((join_kernel<L, decltype(st), decltype(br), true>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
+      else hipLaunchKernelGGL((join_kernel<L, decltype(st), decltype(br), false>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
     });
   });
 }
@@ -479,8 +523,10 @@ hipError_t fade_join_grad_launch(const JoinArgs &a, hipStream_t s) {
         constexpr int L = decltype(l)::value;
         typedef decltype(st) TS;
         typedef decltype(br) TB;
-        if (a.kept) hipLaunchKernelGGL((join_grad_kernel<L, TS, TB, true>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
-        else hipLaunchKernelGGL((join_grad_kernel<L, TS, TB, false>), dim3(blocks), dim3(most(L, 256)), 0, s, a);
+        const bool whole = a.width % 8 == 0;
+        auto *f = a.kept ? (whole ? join_grad_kernel<L, TS, TB, true, true> : join_grad_kernel<L, TS, TB, true, false>)
+                         : (whole ? join_grad_kernel<L, TS, TB, false, true> : join_grad_kernel<L, TS, TB, false, false>);
+        hipLaunchKernelGGL(f, dim3(blocks), dim3(most(L, 256)), 0, s, a);
       });
     });
     if (e != hipSuccess) return e;

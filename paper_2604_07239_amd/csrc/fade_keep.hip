@@ -72,14 +72,12 @@ __device__ __forceinline__ void wg_split(float v, uint32_t &hi, uint32_t &mid, u
   lo = __builtin_bit_cast(uint32_t, rest - __builtin_bit_cast(float, mid));
 }
 __device__ __forceinline__ uint32_t wg_upper(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }  // upper halves, a's first
-// 8 bytes of a checkpoint as bf16, exactly: as unsigned bytes 128 too large, which one instruction each converts, then unit * byte - 128 unit
-__device__ __forceinline__ bf16x8 wg_widen(uint32_t lo, uint32_t hi, uint32_t e) {
-  const float unit = op_keep_unit(e), bias = -128.0f * unit;
-  lo ^= 0x80808080u;
-  hi ^= 0x80808080u;
+__device__ __forceinline__ bf16x8 wg_widen(uint32_t lo, uint32_t hi, uint32_t e) {  // 8 bytes of a checkpoint as bf16, exactly
+  float v[8];
+  op_keep_unpack(make_uint2(lo, hi), op_keep_unit(e), v);
   bf16x8 b;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) b[k] = (bf16_t)fmaf((float)(((k < 4 ? lo : hi) >> ((k & 3) * 8)) & 0xffu), unit, bias);
+  for (int k = 0; k < 8; ++k) b[k] = (bf16_t)v[k];
   return b;
 }
 

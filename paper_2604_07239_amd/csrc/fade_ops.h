@@ -154,7 +154,9 @@ __device__ __forceinline__ uint32_t op_quad_max(uint32_t v) {  // over the four 
   return v > o ? v : o;
 }
 // The 8 bytes of this lane's columns and the group's exponent byte. Every lane of the quad takes part; columns that do not exist hold zeros.
+// x 2^-e + 1.5 * 2^23 is rounded to a whole number, ties to even, whose two's complement is in its low bits: one instruction a value.
 __device__ __forceinline__ uint2 op_keep_pack(const float x[8], uint32_t &e) {
+  // bits of magnitudes are in the magnitudes' order, infinities and NaNs on top
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -164,12 +166,22 @@ __device__ __forceinline__ uint2 op_keep_pack(const float x[8], uint32_t &e) {
   e = op_keep_exp(op_quad_max(top));
   if (e == 255) return make_uint2(0, 0);
   const float inv = __builtin_bit_cast(float, (254u - e) << 23);
-  uint32_t w[2] = {0, 0};
+  uint32_t q[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)(int)rintf(x[i] * inv) & 0xffu) << ((i & 3) * 8);
+  for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, fmaf(x[i], inv, 12582912.0f));
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t a = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400u), b = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400u);
+    w[i] = a | b << 16;
+  }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void op_keep_unpack(const uint2 q, float unit, float x[8]) {
+// As unsigned bytes they are 128 too large, which one instruction each converts, then unit * byte - 128 unit, exactly. An infinite unit gives NaNs.
+__device__ __forceinline__ void op_keep_unpack(uint2 q, float unit, float x[8]) {
+  const float bias = -128.0f * unit;
+  q.x ^= 0x80808080u;
+  q.y ^= 0x80808080u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)(int8_t)((i < 4 ? q.x : q.y) >> ((i & 3) * 8)) * unit;
+  for (int i = 0; i < 8; ++i) x[i] = fmaf((float)(((i < 4 ? q.x : q.y) >> ((i & 3) * 8)) & 0xffu), unit, bias);
 }
