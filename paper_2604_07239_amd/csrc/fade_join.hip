@@ -36,100 +36,75 @@ __device__ __forceinline__ float quotient(float s, float n, float inv) {
   const float q = s * inv;
   return fmaf(fmaf(-n, q, s), inv, q);
 }
-// Sums over the L lanes of a row, the same value in each of them. Above a wavefront through LDS: one barrier a sum, in two places in turn
-// (a wavefront may be one sum ahead of another, never two).
+// What the L lanes of a row know together. Above a wavefront its values pass through LDS: one barrier for four of them, in two places in turn (a wavefront may be
+// one exchange ahead of another, never two).
 template <int L> struct RowSums {
   static constexpr int W = L >= 64 ? L / 64 : 1, GROUPS = L >= 256 ? 1 : 256 / L;  // wavefronts of a row; rows of a workgroup
-  typedef float Lds[2][GROUPS][2][W < 4 ? 4 : W];
+  typedef float Lds[2][GROUPS][4][W];
   Lds &lds;
   int group, wave, width, place = 0;
-  template <int N> __device__ __forceinline__ void sum(float (&v)[N]) {
-    static_assert(N <= 2, "places");
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_total<L>(v[i]);
+  float inv = 1.0f / (float)width;
+  float mine = W > 1 ? fmaxf(columns(wave), 1.0f) : (float)width, inv_mine = 1.0f / mine, theirs = columns(threadIdx.x % W);  // theirs: the wavefront's that this lane reads
+  __device__ __forceinline__ float columns(int w) const {  // of the row's w-th wavefront
+    const int have = width - w * 512, span = (L < 64 ? L : 64) * 8;
+    return (float)(have < 0 ? 0 : have > span ? span : have);
+  }
+  // in: this wavefront's values; out: in lane i those of the row's (i % W)-th wavefront
+  template <int N> __device__ __forceinline__ void exchange(float (&v)[N]) {
     if constexpr (W > 1) {
       if ((threadIdx.x & 63) == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i) lds[place][group][i][wave] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        v[i] = lds[place][group][i][0];
-#pragma unroll
-        for (int w = 1; w < W; ++w) v[i] += lds[place][group][i][w];
-      }
+      for (int i = 0; i < N; ++i) v[i] = lds[place][group][i][threadIdx.x % W];
       place ^= 1;
     }
   }
-  __device__ __forceinline__ float columns(int w) const {  // of the row's w-th wavefront
-    const int have = width - w * 512, span = (L < 64 ? L : 64) * 8;
-    return (float)(have < 0 ? 0 : have > span ? span : have);
+  __device__ __forceinline__ float over_waves(float v) const {  // sum of what exchange() left in the lanes
+    auto add = [](float a, float b) { return a + b; };
+    if constexpr (W >= 16) v = fade_level<8>(v, add);
+    if constexpr (W >= 8) v = fade_level<4>(v, add);
+    if constexpr (W >= 4) v = fade_level<2>(v, add);
+    if constexpr (W >= 2) v = fade_level<1>(v, add);
+    return v;
   }
-  // mean and sum of squared distances from it: centred on the wavefront's own mean, then moved to the row's
-  template <typename F> __device__ __forceinline__ void moments(float s, float inv, float &mean, float &sq, F &&centred) {
-    s = wave_total<L>(s);
-    const float mine = W > 1 ? fmaxf(columns(wave), 1.0f) : (float)width;
-    mean = quotient(s, mine, W > 1 ? __builtin_amdgcn_rcpf(mine) : inv);
-    sq = wave_total<L>(centred(mean));
-    if constexpr (W > 1) {
-      if ((threadIdx.x & 63) == 0) {
-        lds[place][group][0][wave] = mean;
-        lds[place][group][1][wave] = sq;
-      }
-      __syncthreads();
-      float all = 0.0f, m[W];
+  // A row's statistics in two parts: this wavefront's mean m (LayerNorm, else 0) and sum q of squared distances from it; and, of what exchange() left of
+  // them, the row's mean and 1 / sigma: no difference of large squares anywhere.
+  template <bool WHOLE> __device__ __forceinline__ void part(int norm, const float (&x)[8], int left, float &m, float &q) const {
+    m = 0.0f;
+    q = 0.0f;
+    if (norm == FADE_NORM_LAYER) {
+      float s = 0.0f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        m[w] = lds[place][group][0][w];
-        all = fmaf(m[w], columns(w), all);
-      }
-      mean = quotient(all, (float)width, inv);
-      sq = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float d = m[w] - mean;
-        sq += fmaf(d * d, columns(w), lds[place][group][1][w]);
-      }
-      place ^= 1;
-    }
-  }
-};
-
-// statistics of a row's values x: mean (0 unless LayerNorm) and 1 / sigma
-template <int L, bool WHOLE>
-__device__ __forceinline__ void row_stats(RowSums<L> &rs, int norm, const float (&x)[8], int left, float inv, float eps, float &mean, float &rstd) {
-  float sq;
-  if (norm == FADE_NORM_LAYER) {
-    float s = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s += x[k];  // columns that do not exist hold zeros
-    rs.moments(s, inv, mean, sq, [&](float m) {
-      float q = 0.0f;
+      for (int k = 0; k < 8; ++k) s += x[k];  // columns that do not exist hold zeros
+      m = quotient(wave_total<L>(s), mine, inv_mine);
       if (WHOLE || left >= 8 || left <= 0) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float d = x[k] - m;
           q = fmaf(d, d, q);
         }
-        return left > 0 ? q : 0.0f;
-      }
+        q = left > 0 ? q : 0.0f;
+      } else {
 #pragma unroll
-      for (int k = 0; k < 7; ++k) {
-        const float d = x[k] - m;
-        if (k < left) q = fmaf(d, d, q);
+        for (int k = 0; k < 7; ++k) {
+          const float d = x[k] - m;
+          if (k < left) q = fmaf(d, d, q);
+        }
       }
-      return q;
-    });
-  } else {
-    float q[1] = {0.0f};
+    } else if (norm == FADE_NORM_RMS) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) q[0] = fmaf(x[k], x[k], q[0]);
-    rs.sum(q);
-    mean = 0.0f;
-    sq = q[0];
+      for (int k = 0; k < 8; ++k) q = fmaf(x[k], x[k], q);
+    }
+    q = wave_total<L>(q);
   }
-  rstd = __builtin_amdgcn_rsqf(fmaf(sq, inv, eps));  // good to an ulp
-}
+  __device__ __forceinline__ void whole(int norm, float m, float q, float eps, float &mean, float &rstd) const {
+    mean = W > 1 ? quotient(over_waves(m * theirs), (float)width, inv) : m;
+    const float d = m - mean, sq = over_waves(W > 1 ? fmaf(d * d, theirs, q) : q);
+    rstd = norm == FADE_NORM_NONE ? 1.0f : __builtin_amdgcn_rsqf(fmaf(sq, inv, eps));  // good to an ulp
+  }
+};
 
 // 8 columns of a parameter; `otherwise` where there is none, zeros past the row's end
 __device__ __forceinline__ void param8(const float *p, float otherwise, int c, int left, float x[8]) {
@@ -186,8 +161,8 @@ __device__ __forceinline__ void keep_row(uint8_t *keep, int rows, int width, siz
   }
 }
 
-// A workgroup takes rows in strides of the grid; the next rows' operands are on their way while it works on these.
-// WHOLE: the width is a multiple of 8.
+// A workgroup takes rows in strides of the grid. The next rows' operands are on their way while it works on these, and u's statistics of the next rows pass
+// through the same exchange as h's of these: one barrier a row. WHOLE: the width is a multiple of 8.
 template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bounds__(most(L, 256)) void join_kernel(JoinArgs a) {
   typedef RowSums<L> Sums;
   typedef Param<(L <= 512)> P;
@@ -196,7 +171,6 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
   Sums rs{lds, l.group, l.wave(), a.width};
   const P gu(a.gamma_u, 1.0f, l.c, l.left), bu(a.beta_u, 0.0f, l.c, l.left), gn(a.gamma_n, 1.0f, l.c, l.left), bn(a.beta_n, 0.0f, l.c, l.left),
       lam(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c, l.left);
-  const float inv = 1.0f / (float)a.width;
   OpRaw<TS> raw_r;
   OpRaw<TB> raw_u, raw_g;
   raw_r.zero(); raw_u.zero(); raw_g.zero();  // and so they stay in lanes past the row's end
@@ -209,23 +183,31 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
       if (a.g) raw_g.load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c, left);
     }
   };
+  const bool has_n = a.n || a.keep_n;
+  const int norm_n = has_n ? a.norm_n : FADE_NORM_NONE;
   uint32_t base = blockIdx.x * Sums::GROUPS;
+  float x[8], mean_u, rstd_u;
   load(base + l.group);
+  raw_u.get(x);
+  {
+    float v[2];
+    rs.template part<WHOLE>(a.norm_u, x, l.left, v[0], v[1]);
+    if (a.norm_u != FADE_NORM_NONE) rs.exchange(v);
+    rs.whole(a.norm_u, v[0], v[1], a.eps, mean_u, rstd_u);
+  }
   for (; base < (uint32_t)a.rows; base += gridDim.x * Sums::GROUPS) {
     const size_t row = base + l.group;
     const bool in = Sums::GROUPS == 1 || row < (size_t)a.rows;  // the workgroup's barriers are for all its rows
-    float x[8], h[8], g[8], p[8], q[8];
-    raw_u.get(x); raw_r.get(h); raw_g.get(g);
+    float h[8], g[8], p[8], q[8];
+    raw_r.get(h); raw_g.get(g);
     load(row + gridDim.x * Sums::GROUPS);
     if (a.keep_r) keep_row(a.keep_r, a.rows, a.width, row, in, h, l.c);
     if (a.keep_u) keep_row(a.keep_u, a.rows, a.width, row, in, x, l.c);
     if (a.keep_g) keep_row(a.keep_g, a.rows, a.width, row, in, g, l.c);
     if (a.norm_u != FADE_NORM_NONE) {
-      float mean, rstd;
-      row_stats<L, WHOLE>(rs, a.norm_u, x, l.left, inv, a.eps, mean, rstd);
       gu.get(p); bu.get(q);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = fmaf((x[k] - mean) * rstd, p[k], q[k]);
+      for (int k = 0; k < 8; ++k) x[k] = fmaf((x[k] - mean_u) * rstd_u, p[k], q[k]);
     }
     lam.get(p);
 #pragma unroll
@@ -235,10 +217,15 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
       o.put(h);
       o.store(static_cast<TS *>(a.h) + row * a.h_ld + l.c, op_left<WHOLE>(l.left));
     }
-    if (!a.n && !a.keep_n) continue;
-    if (a.norm_n != FADE_NORM_NONE) {
-      float mean, rstd;
-      row_stats<L, WHOLE>(rs, a.norm_n, h, l.left, inv, a.eps, mean, rstd);
+    float v[4], mean, rstd;
+    rs.template part<WHOLE>(norm_n, h, l.left, v[0], v[1]);
+    raw_u.get(x);
+    rs.template part<WHOLE>(a.norm_u, x, l.left, v[2], v[3]);
+    rs.exchange(v);
+    rs.whole(norm_n, v[0], v[1], a.eps, mean, rstd);
+    rs.whole(a.norm_u, v[2], v[3], a.eps, mean_u, rstd_u);
+    if (!has_n) continue;
+    if (norm_n != FADE_NORM_NONE) {
       gn.get(p); bn.get(q);
 #pragma unroll
       for (int k = 0; k < 8; ++k) h[k] = fmaf((h[k] - mean) * rstd, p[k], q[k]);
@@ -279,6 +266,37 @@ struct SavedKeep {  // or from its checkpoint
   __device__ __forceinline__ void get(float x[8]) const { op_keep_unpack(q, op_keep_unit(e), x); }
 };
 
+// A lane's sums over its rows, 8 columns of a parameter: in registers; on rows of 1024 lanes those of the norms' parameters in LDS (128 KB: a row's bytes take
+// the memory longer than these sums take LDS).
+template <int L> struct Sums8 {
+  static constexpr bool LDS = L > 512;
+  float reg[LDS ? 1 : PARTS][8];
+  f32x4 *lds;  // [4][2][L]
+  __device__ __forceinline__ void clear(unsigned char *mem) {
+    lds = reinterpret_cast<f32x4 *>(mem) + threadIdx.x;
+#pragma unroll
+    for (int p = 0; p < (LDS ? 1 : PARTS); ++p)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) reg[p][k] = 0.0f;
+    if constexpr (LDS)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lds[i * L] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  template <int P, typename F> __device__ __forceinline__ void update(F &&f) {  // f(sum, column)
+    if constexpr (LDS && P != PART_LAM) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4 v = lds[(P * 2 + h) * L];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = f(v[k], h * 4 + k);
+        lds[(P * 2 + h) * L] = v;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) reg[LDS ? 0 : P][k] = f(reg[LDS ? 0 : P][k], k);
+    }
+  }
+};
 template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __launch_bounds__(most(L, 256)) void join_grad_kernel(JoinArgs a) {
   typedef RowSums<L> Sums;
   typedef Param<(L <= 512)> P;
@@ -291,12 +309,9 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
   Sums rs{lds, l.group, l.wave(), a.width};
   const P gu(a.gamma_u, 1.0f, l.c, l.left), bu(a.beta_u, 0.0f, l.c, l.left), gn(a.gamma_n, 1.0f, l.c, l.left),
       lam(a.lam_count == 1 ? nullptr : a.lam, a.lam_count == 1 ? a.lam[0] : 1.0f, l.c, l.left);
-  float part[PARTS][8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k)
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) part[p][k] = 0.0f;
-  const float inv = 1.0f / (float)a.width;
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  Sums8<L> part;
+  part.clear(dynamic);
   const void *src_r = KEPT ? a.keep_r : a.r, *src_u = KEPT ? a.keep_u : a.u, *src_g = KEPT ? a.keep_g : a.g;
   RawS raw_r;
   RawB raw_u, raw_g;
@@ -315,68 +330,81 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
       if (a.dn) raw_dn.load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c, left);
     }
   };
+  // Two exchanges a row: h's statistics with the sums of N_n's gradient, and the sums of N_u's with u's statistics of the next row.
   uint32_t base = blockIdx.x * GROUPS;
+  float uhat[8], mean_u, rstd_u;
   load(base + l.group);
+  raw_u.get(uhat);
+  {
+    float v[2];
+    rs.template part<WHOLE>(a.norm_u, uhat, l.left, v[0], v[1]);
+    rs.exchange(v);
+    rs.whole(a.norm_u, v[0], v[1], a.eps, mean_u, rstd_u);
+  }
   for (; base < (uint32_t)a.rows; base += gridDim.x * GROUPS) {
     const size_t row = base + l.group;
     const bool in = GROUPS == 1 || row < (size_t)a.rows;
-    if (!in) none();  // a row that is not there adds zeros
     // forward again: uhat, z, sigma(g), h
-    float uhat[8], z[8], sg[8], r[8], t[8], w[8], rstd_u = 1.0f;
-    raw_u.get(uhat); raw_r.get(r); raw_g.get(sg); raw_dh.get(t);
-    const OpRaw<TB> this_dn = raw_dn;
+    float z[8], sg[8], r[8], t[8], e[8], w[8];
+    raw_r.get(r); raw_g.get(sg); raw_dh.get(t); raw_dn.get(e);
     load(row + gridDim.x * GROUPS);
+    if (!in)  // a row that is not there adds zeros
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[k] = sg[k] = t[k] = e[k] = uhat[k] = 0.0f;
     if (a.norm_u != FADE_NORM_NONE) {
-      float mean, q[8];
-      row_stats<L, WHOLE>(rs, a.norm_u, uhat, l.left, inv, a.eps, mean, rstd_u);
+      float q[8];
       gu.get(w); bu.get(q);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        uhat[k] = (uhat[k] - mean) * rstd_u;
+        uhat[k] = (uhat[k] - mean_u) * rstd_u;
         z[k] = fmaf(uhat[k], w[k], q[k]);
       }
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) z[k] = uhat[k];
     }
+    if (src_g)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sg[k] = src_g ? sigma(sg[k]) : 1.0f;
+      for (int k = 0; k < 8; ++k) sg[k] = sigma(sg[k]);
+    else
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sg[k] = 1.0f;
     // t = dh + N_n'(dn)
-    if (a.dn) {
-      float e[8];
-      this_dn.get(e);
-      if (a.norm_n != FADE_NORM_NONE) {
-        float h[8], mean, rstd, s[2] = {0.0f, 0.0f};
-        lam.get(w);
+    if (a.dn && a.norm_n != FADE_NORM_NONE) {
+      float h[8], v[4], mean, rstd;
+      lam.get(w);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) h[k] = fmaf(w[k], r[k], sg[k] * z[k]);
-        row_stats<L, WHOLE>(rs, a.norm_n, h, l.left, inv, a.eps, mean, rstd);
-        gn.get(w);
+      for (int k = 0; k < 8; ++k) h[k] = fmaf(w[k], r[k], sg[k] * z[k]);
+      rs.template part<WHOLE>(a.norm_n, h, l.left, v[0], v[1]);
+      part.template update<PART_BN>([&](float s, int k) { return s + e[k]; });
+      gn.get(w);
+      const float m = v[0];
+      float e0 = 0.0f, e1 = 0.0f;  // sums of e = dn gamma and of e times h's distance from the wavefront's mean
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          h[k] = (h[k] - mean) * rstd;
-          part[PART_GN][k] = fmaf(e[k], h[k], part[PART_GN][k]);
-          part[PART_BN][k] += e[k];
-          e[k] *= w[k];
-          s[0] += e[k];
-          s[1] = fmaf(e[k], h[k], s[1]);
-        }
-        rs.sum(s);
-        const float level = a.norm_n == FADE_NORM_LAYER ? s[0] * inv : 0.0f, along = s[1] * inv;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = fmaf(rstd, fmaf(-h[k], along, e[k] - level), t[k]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] += e[k];
+      for (int k = 0; k < 8; ++k) {
+        const float f = e[k] * w[k];
+        e0 += f;
+        e1 = fmaf(f, h[k] - m, e1);
       }
+      v[2] = wave_total<L>(e0);
+      v[3] = wave_total<L>(e1);
+      rs.exchange(v);
+      rs.whole(a.norm_n, v[0], v[1], a.eps, mean, rstd);
+      const float along = rs.over_waves(fmaf(v[0] - mean, v[2], v[3])) * rstd * rs.inv, level = a.norm_n == FADE_NORM_LAYER ? rs.over_waves(v[2]) * rs.inv : 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) h[k] = (h[k] - mean) * rstd;
+      part.template update<PART_GN>([&](float s, int k) { return fmaf(e[k], h[k], s); });
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = fmaf(rstd, fmaf(-h[k], along, fmaf(e[k], w[k], -level)), t[k]);
+    } else if (a.dn) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] += e[k];
     }
     // through the join
     lam.get(w);
+    part.template update<PART_LAM>([&](float s, int k) { return fmaf(t[k], r[k], s); });
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      part[PART_LAM][k] = fmaf(t[k], r[k], part[PART_LAM][k]);
-      r[k] = w[k] * t[k];
-    }
+    for (int k = 0; k < 8; ++k) r[k] = w[k] * t[k];
     const bool store = in && l.left > 0;
     if (a.dr && store) {
       OpRaw<TS> o;
@@ -394,56 +422,72 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
       o.store(static_cast<TB *>(a.dg) + row * a.dg_ld + l.c, op_left<WHOLE>(l.left));
     }
     // du = N_u'(dz)
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f}, rstd = rstd_u, x[8];
     if (a.norm_u != FADE_NORM_NONE) {
-      float s[2] = {0.0f, 0.0f};
       gu.get(w);
+      part.template update<PART_GU>([&](float s, int k) { return fmaf(t[k], uhat[k], s); });
+      part.template update<PART_BU>([&](float s, int k) { return s + t[k]; });
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        part[PART_GU][k] = fmaf(t[k], uhat[k], part[PART_GU][k]);
-        part[PART_BU][k] += t[k];
         t[k] *= w[k];
-        s[0] += t[k];
-        s[1] = fmaf(t[k], uhat[k], s[1]);
+        v[0] += t[k];
+        v[1] = fmaf(t[k], uhat[k], v[1]);
       }
-      rs.sum(s);
-      const float level = a.norm_u == FADE_NORM_LAYER ? s[0] * inv : 0.0f, along = s[1] * inv;
+      v[0] = wave_total<L>(v[0]);
+      v[1] = wave_total<L>(v[1]);
+    }
+    raw_u.get(x);
+    rs.template part<WHOLE>(a.norm_u, x, l.left, v[2], v[3]);
+    rs.exchange(v);
+    rs.whole(a.norm_u, v[2], v[3], a.eps, mean_u, rstd_u);
+    if (a.norm_u != FADE_NORM_NONE) {
+      const float level = a.norm_u == FADE_NORM_LAYER ? rs.over_waves(v[0]) * rs.inv : 0.0f, along = rs.over_waves(v[1]) * rs.inv;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) t[k] = rstd_u * fmaf(-uhat[k], along, t[k] - level);
+      for (int k = 0; k < 8; ++k) t[k] = rstd * fmaf(-uhat[k], along, t[k] - level);
     }
     if (a.du && store) {
       OpRaw<TB> o;
       o.put(t);
       o.store(static_cast<TB *>(a.du) + row * a.du_ld + l.c, op_left<WHOLE>(l.left));
     }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) uhat[k] = x[k];
   }
   // the workgroup's sums over its rows, its groups' in order
   if (a.lam_count == 1) {
     float s[1] = {0.0f};
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[0] += part[PART_LAM][k];
-    rs.sum(s);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) part[PART_LAM][k] = s[0];
+    part.template update<PART_LAM>([&](float v, int) { s[0] += v; return v; });
+    s[0] = wave_total<L>(s[0]);
+    rs.exchange(s);
+    s[0] = rs.over_waves(s[0]);
+    part.template update<PART_LAM>([&](float, int) { return s[0]; });
   }
   float *dst = a.work + (size_t)blockIdx.x * PARTS * part_width(a.width);
-#pragma unroll
-  for (int p = 0; p < PARTS; ++p) {
+  auto leave = [&](auto p_c) {
+    constexpr int p = decltype(p_c)::value;
+    float x[8];
+    part.template update<p>([&](float v, int k) { x[k] = v; return v; });
     if constexpr (GROUPS > 1) {
       __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) fold[(l.group * 8 + k) * L + l.lane] = part[p][k];
+      for (int k = 0; k < 8; ++k) fold[(l.group * 8 + k) * L + l.lane] = x[k];
       __syncthreads();
       if (l.group == 0)
         for (int g = 1; g < GROUPS; ++g)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) part[p][k] += fold[(g * 8 + k) * L + l.lane];
+          for (int k = 0; k < 8; ++k) x[k] += fold[(g * 8 + k) * L + l.lane];
     }
     if (l.group == 0 && l.left > 0) {
       OpRaw<float> o;
-      o.put(part[p]);
+      o.put(x);
       o.store(dst + p * part_width(a.width) + l.c, 8);
     }
-  }
+  };
+  leave(std::integral_constant<int, PART_GU>{});
+  leave(std::integral_constant<int, PART_BU>{});
+  leave(std::integral_constant<int, PART_GN>{});
+  leave(std::integral_constant<int, PART_BN>{});
+  leave(std::integral_constant<int, PART_LAM>{});
 }
 
 // The workgroups' partial sums, in order: 64 columns of one parameter a workgroup, four a lane, 64 slices of the partial sums side by side, then the slices in four
@@ -526,7 +570,9 @@ hipError_t fade_join_grad_launch(const JoinArgs &a, hipStream_t s) {
         const bool whole = a.width % 8 == 0;
         auto *f = a.kept ? (whole ? join_grad_kernel<L, TS, TB, true, true> : join_grad_kernel<L, TS, TB, true, false>)
                          : (whole ? join_grad_kernel<L, TS, TB, false, true> : join_grad_kernel<L, TS, TB, false, false>);
-        hipLaunchKernelGGL(f, dim3(blocks), dim3(most(L, 256)), 0, s, a);
+        constexpr int LDS = Sums8<L>::LDS ? 8 * L * 16 : 0;
+        if (LDS) (void)hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        hipLaunchKernelGGL(f, dim3(blocks), dim3(most(L, 256)), LDS, s, a);
       });
     });
     if (e != hipSuccess) return e;
