@@ -61,13 +61,16 @@ __global__ __launch_bounds__(256) void sort_count_kernel(OpTokens t, GradPlan p,
   for (uint32_t d = threadIdx.x; d < digits; d += 256) count[d] = 0;
   __syncthreads();
   const uint32_t n = FIRST ? p.n : total[MAX_DIGITS];
-  const size_t begin = (size_t)blockIdx.x * 256 * p.items;
-  for (int i = 0; i < p.items; ++i) {
+  const size_t begin = (size_t)blockIdx.x * (256 * SORT_ITEMS);
+  uint32_t k[SORT_ITEMS];
+#pragma unroll
+  for (int i = 0; i < SORT_ITEMS; ++i) {
     const size_t at = begin + i * 256 + threadIdx.x;
-    if (at >= n) break;
-    const uint32_t k = FIRST ? token_at(t, at, p.vocab) : keys[at];
-    if (k != NO_TOKEN) atomicAdd(&count[(k >> low) & (digits - 1)], 1u);
+    k[i] = at >= n ? NO_TOKEN : FIRST ? token_at(t, at, p.vocab) : keys[at];
   }
+#pragma unroll
+  for (int i = 0; i < SORT_ITEMS; ++i)
+    if (k[i] != NO_TOKEN) atomicAdd(&count[(k[i] >> low) & (digits - 1)], 1u);
   __syncthreads();
   for (uint32_t d = threadIdx.x; d < digits; d += 256) hist[(size_t)d * p.tiles + blockIdx.x] = count[d];
   if (FIRST) {
@@ -98,73 +101,79 @@ __global__ __launch_bounds__(256) void sort_place_kernel(OpTokens t, GradPlan p,
   __shared__ uint32_t count[4][MAX_DIGITS];  // per wavefront, then where its first element of the digit goes
   __shared__ uint32_t wave_sum[4];
   const uint32_t digits = 1u << p.bits;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (uint32_t d = tid; d < 4 * MAX_DIGITS; d += 256) count[d / MAX_DIGITS][d % MAX_DIGITS] = 0;
-  __syncthreads();
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (int)((digits + 255) / 256);  // digits per thread, at most 4
+  // everything that has to come from memory, at once
   const uint32_t n = FIRST ? p.n : total[MAX_DIGITS];
-  const size_t begin = (size_t)blockIdx.x * 256 * p.items + (size_t)wave * 64 * p.items;
-  uint32_t key[16], rank[16];
+  const size_t begin = (size_t)blockIdx.x * (256 * SORT_ITEMS) + (size_t)wave * (64 * SORT_ITEMS);
+  uint32_t key[SORT_ITEMS], at_pos[SORT_ITEMS], rank[SORT_ITEMS], all[4], front[4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < SORT_ITEMS; ++i) {
+    const size_t at = begin + i * 64 + lane;
     key[i] = NO_TOKEN;
-    if (i < p.items) {
-      const size_t at = begin + i * 64 + lane;
-      if (at < n) key[i] = FIRST ? token_at(t, at, p.vocab) : keys[at];
+    at_pos[i] = (uint32_t)at;
+    if (at < n) {
+      key[i] = FIRST ? token_at(t, at, p.vocab) : keys[at];
+      if (!FIRST) at_pos[i] = pos[at];
     }
   }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    rank[i] = 0;
-    if (i < p.items) {
-      const bool in = key[i] != NO_TOKEN;
-      const uint32_t d = (key[i] >> low) & (digits - 1);
-      uint64_t same = __ballot(in);
-      for (int b = 0; b < p.bits; ++b) {
-        const bool one = (d >> b) & 1;
-        const uint64_t m = __ballot(one);
-        same &= one ? m : ~m;
-      }
-      const uint64_t below = same & (((uint64_t)1 << lane) - 1);
-      if (in) rank[i] = count[wave][d] + (uint32_t)__popcll(below);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (in && below == 0) count[wave][d] += (uint32_t)__popcll(same);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
-  }
-  __syncthreads();
-  // digits in front: an exclusive scan of the totals, four digits per thread
-  uint32_t v[4], sum = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t d = tid * 4 + j;
-    v[j] = sum;
-    sum += d < digits ? total[d] : 0;
+    const uint32_t d = tid * per + j;
+    const bool in = j < per && d < digits;
+    all[j] = in ? total[d] : 0;
+    front[j] = in ? hist[(size_t)d * p.tiles + blockIdx.x] : 0;
   }
+  for (uint32_t d = tid; d < digits; d += 256)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) count[w][d] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SORT_ITEMS; ++i) {
+    const bool in = key[i] != NO_TOKEN;
+    const uint32_t d = (key[i] >> low) & (digits - 1);
+    uint64_t same = __ballot(in);
+    for (int b = 0; b < p.bits; ++b) {
+      const bool one = (d >> b) & 1;
+      const uint64_t m = __ballot(one);
+      same &= one ? m : ~m;
+    }
+    const uint64_t below = same & (((uint64_t)1 << lane) - 1);
+    rank[i] = 0;
+    if (in) rank[i] = count[wave][d] + (uint32_t)__popcll(below);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (in && below == 0) count[wave][d] += (uint32_t)__popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  // digits in front: an exclusive scan of the totals
+  uint32_t sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum += all[j];
   const uint32_t upto = fade_lanes_scan(sum);
   if (lane == 63) wave_sum[wave] = upto;
   __syncthreads();
   uint32_t before = upto - sum;
   for (int w = 0; w < wave; ++w) before += wave_sum[w];
+  if (FIRST && blockIdx.x == 0 && tid == 255) total[MAX_DIGITS] = before + sum;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t d = tid * 4 + j;
-    if (d >= digits) break;
-    uint32_t to = before + v[j] + hist[(size_t)d * p.tiles + blockIdx.x];
+    const uint32_t d = tid * per + j;
+    if (j >= per || d >= digits) break;
+    uint32_t to = before + front[j];
+    before += all[j];
+#pragma unroll
     for (int w = 0; w < 4; ++w) {
       const uint32_t c = count[w][d];
       count[w][d] = to;
       to += c;
     }
   }
-  if (FIRST && blockIdx.x == 0 && tid == 255) total[MAX_DIGITS] = before + sum;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (i < p.items && key[i] != NO_TOKEN) {
-      const size_t at = begin + i * 64 + lane;
+  for (int i = 0; i < SORT_ITEMS; ++i)
+    if (key[i] != NO_TOKEN) {
       const uint32_t to = count[wave][(key[i] >> low) & (digits - 1)] + rank[i];
       keys_out[to] = key[i];
-      pos_out[to] = FIRST ? (uint32_t)at : pos[at];
+      pos_out[to] = at_pos[i];
       if (LAST) flags[key[i]] = 1;
     }
 }
@@ -172,15 +181,10 @@ __global__ __launch_bounds__(256) void sort_place_kernel(OpTokens t, GradPlan p,
 // ---------------------------------------------------------------------------------------------------
 // The sums
 // ---------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void grad_clear_kernel(GradPlan p, const uint8_t *flags, float *grad, size_t grad_ld, int width) {
-  const size_t v = (size_t)blockIdx.x * (256 >> p.shift) + (threadIdx.x >> p.shift);
-  if (v >= p.vocab || flags[v]) return;
-  OpRaw<float> o;
-  o.zero();
-  for (int c = (threadIdx.x & ((1 << p.shift) - 1)) * 8; c < width; c += 8 << p.shift) o.store(grad + v * grad_ld + c, width - c);
-}
 struct SumArgs {
   const uint32_t *keys, *pos, *total;
+  const uint8_t *flags;  // tokens that occur
+  uint32_t clears;       // workgroups that write the rows of the others
   const void *dout;
   size_t dout_ld;
   float scale;
@@ -205,18 +209,46 @@ __device__ __forceinline__ void grad_put(const SumArgs &a, uint32_t v, int c, fl
   o.put(x);
   o.store(dst, a.width - c);
 }
-template <typename T> __global__ __launch_bounds__(256) void grad_sum_kernel(GradPlan p, SumArgs a) {
-  const uint32_t g = blockIdx.x * (256 >> p.shift) + (threadIdx.x >> p.shift);
+// The first workgroups write zeros into the rows of tokens that do not occur, which is bounded by the memory's writes; the others wait for reads, and the two
+// share the chip.
+// FULL: a group of lanes is a wavefront; its positions and keys come with one load each and go round as scalars.
+template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum_kernel(GradPlan p, SumArgs a) {
+  if (blockIdx.x < a.clears) {
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int lanes = 1 << p.shift, first = (threadIdx.x & (lanes - 1)) * 4;
+    for (size_t v = (size_t)blockIdx.x * (256 >> p.shift) + (threadIdx.x >> p.shift); v < p.vocab; v += (size_t)a.clears * (256 >> p.shift)) {
+      if (a.flags[v]) continue;
+      float *dst = a.grad + v * a.grad_ld;
+      int c = first;
+      for (; c + 4 <= a.width; c += lanes * 4) *reinterpret_cast<op_f32x4 *>(dst + c) = zero;
+      for (int k = c; k < a.width && k < c + 4; ++k) dst[k] = 0.0f;
+    }
+    return;
+  }
+  uint32_t g = (blockIdx.x - a.clears) * (256 >> p.shift) + (threadIdx.x >> p.shift);
+  if constexpr (FULL) g = __builtin_amdgcn_readfirstlane(g);
   const uint32_t piece = g / p.strips;
   const int c = ((g - piece * p.strips) << (p.shift + 3)) + (threadIdx.x & ((1 << p.shift) - 1)) * 8;
   const uint32_t n = a.total[MAX_DIGITS];
   const size_t first = (size_t)piece * p.piece;
-  if (first >= n || c >= a.width) return;
-  const uint32_t begin = (uint32_t)first, end = n - begin < p.piece ? n : begin + p.piece;
-  uint32_t cur = a.keys[begin];
-  bool came = begin > 0 && a.keys[begin - 1] == cur;
+  if (first >= n || (!FULL && c >= a.width)) return;
+  const uint32_t begin = (uint32_t)first, end = n - begin < p.piece ? n : begin + p.piece, lane = threadIdx.x & 63;
+  // FULL: lane i has the i-th position of the piece (at most 62 of them), lanes 63 and 62 the keys on either side
+  uint32_t my_key = 0, my_pos = 0;
+  if constexpr (FULL) {
+    const uint32_t at = lane == 63 ? (begin > 0 ? begin - 1 : 0) : lane == 62 ? (end < n ? end : end - 1) : begin + lane < end ? begin + lane : end - 1;
+    my_key = a.keys[at];
+    my_pos = a.pos[at];
+  }
+  auto key_at = [&](uint32_t i) { return FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_key, (int)(i - begin)) : a.keys[i]; };
+  auto pos_at = [&](uint32_t i) { return FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_pos, (int)(i - begin)) : a.pos[i]; };
+  const uint32_t before = FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_key, 63) : a.keys[begin > 0 ? begin - 1 : 0];
+  const uint32_t behind = FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_key, 62) : a.keys[end < n ? end : end - 1];
+  uint32_t cur = key_at(begin);
+  bool came = begin > 0 && before == cur;
   float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   auto leave = [&](bool goes) {  // the run that ends here, or at the piece's end
+    if (c >= a.width) return;
     if (came || goes) {
       OpRaw<float> o;
       o.put(acc);
@@ -225,18 +257,20 @@ template <typename T> __global__ __launch_bounds__(256) void grad_sum_kernel(Gra
       grad_put(a, cur, c, acc);
     }
   };
-  const T *src = static_cast<const T *>(a.dout) + c;
-  for (uint32_t i = begin; i < end; i += 4) {
-    uint32_t key[4];
-    OpRaw<T> row[4];
+  constexpr uint32_t AHEAD = 8;  // rows on their way at a time
+  const T *src = static_cast<const T *>(a.dout) + (c < a.width ? c : 0);
+  const int left = c < a.width ? a.width - c : 8;
+  for (uint32_t i = begin; i < end; i += AHEAD) {
+    uint32_t key[AHEAD];
+    OpRaw<T> row[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (uint32_t j = 0; j < AHEAD; ++j) {
       const uint32_t at = i + j < end ? i + j : end - 1;
-      key[j] = a.keys[at];
-      row[j].load(src + a.pos[at] * a.dout_ld, a.width - c);
+      key[j] = key_at(at);
+      row[j].load(src + pos_at(at) * a.dout_ld, left);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (uint32_t j = 0; j < AHEAD; ++j) {
       if (i + j >= end) break;
       if (key[j] != cur) {
         leave(false);
@@ -251,7 +285,7 @@ template <typename T> __global__ __launch_bounds__(256) void grad_sum_kernel(Gra
       for (int k = 0; k < 8; ++k) acc[k] += x[k];
     }
   }
-  leave(end < n && a.keys[end] == cur);
+  leave(end < n && behind == cur);
 }
 // The runs that cross pieces: the workgroup of the piece a run starts in adds its partial sums, its groups of lanes in equal ranges of the pieces
 // in between, then the groups' sums in order.
@@ -284,7 +318,20 @@ __global__ __launch_bounds__(256) void grad_join_kernel(GradPlan p, SumArgs a) {
   };
   if (c < a.width) {
     if (group == 0) add(piece, 1);
-    for (uint32_t i = from; i < to; ++i) add(i, 0);
+    uint32_t i = from;
+    for (; i + 8 <= to; i += 8) {
+      OpRaw<float> o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j].load(a.part + (size_t)(i + j) * 2 * a.part_ld + c, 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float x[8];
+        o[j].get(x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] += x[k];
+      }
+    }
+    for (; i < to; ++i) add(i, 0);
   }
 #pragma unroll
   for (int k = 0; k < 8; ++k) sums[threadIdx.x][k] = acc[k];
@@ -343,15 +390,13 @@ hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout
       hipLaunchKernelGGL((sort_place_kernel<false, true>), tiles, b, 0, s, t, p, k1, p1, hist, total, k0, p0, flags, p.bits);
     }
   }
-  const int groups = 256 >> p.shift;
-  if (!accumulate)
-    hipLaunchKernelGGL(grad_clear_kernel, dim3((uint32_t)((vocab + groups - 1) / groups)), b, 0, s, p, flags, grad, grad_ld, (int)width);
-  if (n) {
-    SumArgs a{k0, p0, total, dout.p, dout.ld, scale, grad, grad_ld, reinterpret_cast<float *>(w + p.part), (int)width, (int)((width + 7) & ~(size_t)7), accumulate};
-    const dim3 sums((uint32_t)(((size_t)p.pieces * p.strips + groups - 1) / groups));
-    if (dout.f32) hipLaunchKernelGGL(grad_sum_kernel<float>, sums, b, 0, s, p, a);
-    else hipLaunchKernelGGL(grad_sum_kernel<bf16_t>, sums, b, 0, s, p, a);
-    if (p.pieces > 1) hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)((size_t)p.pieces * p.strips)), b, 0, s, p, a);
-  }
+  const uint32_t groups = 256 >> p.shift, rows = (uint32_t)((vocab + groups - 1) / groups), clears = accumulate ? 0 : rows < 256 ? rows : 256;
+  const SumArgs a{k0, p0, total, flags, clears, dout.p, dout.ld, scale, grad, grad_ld, reinterpret_cast<float *>(w + p.part), (int)width, (int)((width + 7) & ~(size_t)7),
+                  accumulate};
+  const dim3 sums(clears + (uint32_t)(((size_t)p.pieces * p.strips + groups - 1) / groups));
+  auto *sum = dout.f32 ? (p.shift == 6 ? grad_sum_kernel<float, true> : grad_sum_kernel<float, false>)
+                       : (p.shift == 6 ? grad_sum_kernel<bf16_t, true> : grad_sum_kernel<bf16_t, false>);
+  hipLaunchKernelGGL(sum, sums, b, 0, s, p, a);
+  if (p.pieces > 1) hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)((size_t)p.pieces * p.strips)), b, 0, s, p, a);
   return hipGetLastError();
 }

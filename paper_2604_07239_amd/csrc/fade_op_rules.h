@@ -8,13 +8,13 @@
 namespace fade_op {
 
 struct GradPlan {
-  int passes, bits, items;      // digits; elements per thread of a tile of 256 threads
+  int passes, bits;             // digits
   uint32_t n, vocab, tiles;
   int shift, strips;            // 2^shift lanes on a strip of columns, 8 each
-  uint32_t piece, pieces;       // sorted positions summed by one group of lanes
+  uint32_t piece, pieces;       // sorted positions summed by one group of lanes, at most 62
   size_t keys[2], pos[2], hist, total, flags, part, bytes;
 };
-constexpr int MAX_DIGITS = 1024;
+constexpr int MAX_DIGITS = 1024, SORT_ITEMS = 4;  // elements per thread of a tile of 256 threads
 
 inline int lanes_shift(size_t width, int most) {  // lanes for a row of this width: the least power of two that covers it, at most 2^most
   int s = 2;
@@ -29,11 +29,12 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
   p.bits = (bits + p.passes - 1) / p.passes;
   p.n = (uint32_t)n;
   p.vocab = (uint32_t)vocab;
-  p.items = n <= ((size_t)1 << 17) ? 4 : 16;
-  p.tiles = n ? (uint32_t)((n + 256 * p.items - 1) / (256 * p.items)) : 1;
+  p.tiles = n ? (uint32_t)((n + 256 * SORT_ITEMS - 1) / (256 * SORT_ITEMS)) : 1;
   p.shift = lanes_shift(width, 6);
   p.strips = (int)((width + ((size_t)8 << p.shift) - 1) / ((size_t)8 << p.shift));
-  p.piece = 32;
+  // as many pieces as there are wavefronts for, but none so short that the partial sums at their borders cost more than the rows between
+  const size_t want = n * p.strips >> (6 - p.shift);
+  p.piece = (uint32_t)(want >= (size_t)1 << 18 ? 60 : want >= (size_t)1 << 17 ? 32 : want >= (size_t)1 << 15 ? 16 : 8);
   p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
   size_t at = 0;
   auto take = [&](size_t bytes) {

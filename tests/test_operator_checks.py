@@ -176,7 +176,7 @@ int main() {
         const GradPlan p = grad_plan(n, vocab, width);
         // the digits cover every token, the tiles and pieces every position, the lanes every column, and no region of the workspace another
         WANT(p.passes * p.bits <= 20 && ((size_t)1 << (p.passes * p.bits)) >= vocab && (1 << p.bits) <= MAX_DIGITS);
-        WANT(p.items <= 16 && (size_t)p.tiles * 256 * p.items >= n && p.tiles >= 1);
+        WANT((size_t)p.tiles * 256 * SORT_ITEMS >= n && p.tiles >= 1);
         WANT((size_t)p.pieces * p.piece >= n);
         WANT(((size_t)p.strips * 8 << p.shift) >= width && p.shift >= 2 && p.shift <= 6);
         size_t at = 0;
