@@ -209,71 +209,93 @@ __device__ __forceinline__ void grad_put(const SumArgs &a, uint32_t v, int c, fl
   o.put(x);
   o.store(dst, a.width - c);
 }
+// Pieces of the sorted positions, one group of lanes each for a strip of columns. A run (the positions of one token) belongs to the piece it starts in, which
+// follows it into the next piece if it ends there; a longer one leaves the sums of its parts to grad_join_kernel.
+// FULL: a group of lanes is a wavefront; its positions and keys come with a few loads and go round as scalars.
 // The first workgroups write zeros into the rows of tokens that do not occur, which is bounded by the memory's writes; the others wait for reads, and the two
 // share the chip.
-// FULL: a group of lanes is a wavefront; its positions and keys come with one load each and go round as scalars.
 template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum_kernel(GradPlan p, SumArgs a) {
-  if (blockIdx.x < a.clears) {
-    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int lanes = 1 << p.shift, first = (threadIdx.x & (lanes - 1)) * 4;
-    for (size_t v = (size_t)blockIdx.x * (256 >> p.shift) + (threadIdx.x >> p.shift); v < p.vocab; v += (size_t)a.clears * (256 >> p.shift)) {
-      if (a.flags[v]) continue;
-      float *dst = a.grad + v * a.grad_ld;
-      int c = first;
-      for (; c + 4 <= a.width; c += lanes * 4) *reinterpret_cast<op_f32x4 *>(dst + c) = zero;
-      for (int k = c; k < a.width && k < c + 4; ++k) dst[k] = 0.0f;
+  const uint32_t lane = threadIdx.x & 63;
+  if (blockIdx.x < a.clears) {  // 64 rows of the table per wavefront and turn
+    const op_f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int lanes = 1 << p.shift, first = (threadIdx.x & (lanes - 1)) * 4, rows = 64 >> p.shift, mine = (int)lane >> p.shift;
+    for (uint32_t v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; v0 < p.vocab; v0 += a.clears * 256) {
+      const uint64_t absent = __ballot(v0 + lane < p.vocab && !a.flags[v0 + lane]);
+      for (int r = 0; r < 64; r += rows) {
+        if (!(absent >> (r + mine) & 1)) continue;
+        float *dst = a.grad + (size_t)(v0 + r + mine) * a.grad_ld;
+        int c = first;
+        for (; c + 4 <= a.width; c += lanes * 4) __builtin_nontemporal_store(zero, reinterpret_cast<op_f32x4 *>(dst + c));
+        for (int k = c; k < a.width && k < c + 4; ++k) dst[k] = 0.0f;
+      }
     }
     return;
   }
   uint32_t g = (blockIdx.x - a.clears) * (256 >> p.shift) + (threadIdx.x >> p.shift);
   if constexpr (FULL) g = __builtin_amdgcn_readfirstlane(g);
-  const uint32_t piece = g / p.strips;
+  const uint32_t piece = g / p.strips, P = p.piece;
   const int c = ((g - piece * p.strips) << (p.shift + 3)) + (threadIdx.x & ((1 << p.shift) - 1)) * 8;
   const uint32_t n = a.total[MAX_DIGITS];
-  const size_t first = (size_t)piece * p.piece;
+  const size_t first = (size_t)piece * P;
   if (first >= n || (!FULL && c >= a.width)) return;
-  const uint32_t begin = (uint32_t)first, end = n - begin < p.piece ? n : begin + p.piece, lane = threadIdx.x & 63;
-  // FULL: lane i has the i-th position of the piece (at most 62 of them), lanes 63 and 62 the keys on either side
-  uint32_t my_key = 0, my_pos = 0;
+  const uint32_t begin = (uint32_t)first, end = n - begin < P ? n : begin + P, last = n - 1;
+  auto inside = [&](uint32_t i) { return i < last ? i : last; };
+  // FULL: lane i has the i-th position of the piece and of the next one (at most 60 of them), and the keys at the borders
+  uint32_t my_key = 0, my_pos = 0, next_key = 0, next_pos = 0;
   if constexpr (FULL) {
-    const uint32_t at = lane == 63 ? (begin > 0 ? begin - 1 : 0) : lane == 62 ? (end < n ? end : end - 1) : begin + lane < end ? begin + lane : end - 1;
-    my_key = a.keys[at];
+    const uint32_t at = inside(begin + (lane < P ? lane : P - 1)), next = inside(end + lane);
+    my_key = a.keys[lane == 63 ? (begin > 0 ? begin - 1 : 0) : lane == 62 ? (begin > P ? begin - P - 1 : 0) : at];
     my_pos = a.pos[at];
+    next_key = a.keys[next];
+    next_pos = a.pos[next];
   }
-  auto key_at = [&](uint32_t i) { return FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_key, (int)(i - begin)) : a.keys[i]; };
-  auto pos_at = [&](uint32_t i) { return FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_pos, (int)(i - begin)) : a.pos[i]; };
-  const uint32_t before = FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_key, 63) : a.keys[begin > 0 ? begin - 1 : 0];
-  const uint32_t behind = FULL ? (uint32_t)__builtin_amdgcn_readlane((int)my_key, 62) : a.keys[end < n ? end : end - 1];
+  auto lane_of = [](uint32_t v, uint32_t i) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)i); };
+  auto key_at = [&](uint32_t i) { return FULL ? lane_of(my_key, i - begin) : a.keys[i]; };
+  const uint32_t before = FULL ? lane_of(my_key, 63) : a.keys[begin > 0 ? begin - 1 : 0], far_before = FULL ? lane_of(my_key, 62) : a.keys[begin > P ? begin - P - 1 : 0];
+  const uint32_t behind = FULL ? lane_of(next_key, 0) : a.keys[inside(end)], far_behind = FULL ? lane_of(next_key, P) : a.keys[inside(end + P)];
+  const uint32_t last_key = key_at(end - 1);
   uint32_t cur = key_at(begin);
   bool came = begin > 0 && before == cur;
+  const bool goes = end < n && behind == last_key;                                  // the last run does not end here
+  const bool far = goes && end + P < n && far_behind == last_key;                   // nor in the next piece
+  const bool from_far = came && begin > P && far_before == cur;                     // the first run does not start in the piece in front
   float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  auto leave = [&](bool goes) {  // the run that ends here, or at the piece's end
+  auto part = [&](int which) {
     if (c >= a.width) return;
-    if (came || goes) {
-      OpRaw<float> o;
-      o.put(acc);
-      o.store(a.part + ((size_t)piece * 2 + (came ? 0 : 1)) * a.part_ld + c, 8);
-    } else {
-      grad_put(a, cur, c, acc);
-    }
+    OpRaw<float> o;
+    o.put(acc);
+    o.store(a.part + ((size_t)piece * 2 + which) * a.part_ld + c, 8);
   };
   constexpr uint32_t AHEAD = 8;  // rows on their way at a time
   const T *src = static_cast<const T *>(a.dout) + (c < a.width ? c : 0);
   const int left = c < a.width ? a.width - c : 8;
-  for (uint32_t i = begin; i < end; i += AHEAD) {
+  uint32_t i = begin;
+  if (came && !from_far && !(goes && last_key == cur)) {  // the piece in front follows its run to the end
+    if constexpr (FULL) {
+      const uint64_t other = __ballot(my_key != cur && lane < end - begin);
+      i = other ? begin + (uint32_t)__builtin_ctzll(other) : end;
+    } else {
+      while (i < end && a.keys[i] == cur) ++i;
+    }
+    if (i == end) return;
+    cur = key_at(i);
+    came = false;
+  }
+  for (; i < end; i += AHEAD) {
     uint32_t key[AHEAD];
     OpRaw<T> row[AHEAD];
 #pragma unroll
     for (uint32_t j = 0; j < AHEAD; ++j) {
       const uint32_t at = i + j < end ? i + j : end - 1;
       key[j] = key_at(at);
-      row[j].load(src + pos_at(at) * a.dout_ld, left);
+      row[j].load(src + (FULL ? lane_of(my_pos, at - begin) : a.pos[at]) * a.dout_ld, left);
     }
 #pragma unroll
     for (uint32_t j = 0; j < AHEAD; ++j) {
       if (i + j >= end) break;
       if (key[j] != cur) {
-        leave(false);
+        if (came) part(0);
+        else if (c < a.width) grad_put(a, cur, c, acc);
         cur = key[j];
         came = false;
 #pragma unroll
@@ -285,62 +307,110 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
       for (int k = 0; k < 8; ++k) acc[k] += x[k];
     }
   }
-  leave(end < n && behind == cur);
-}
-// The runs that cross pieces: the workgroup of the piece a run starts in adds its partial sums, its groups of lanes in equal ranges of the pieces
-// in between, then the groups' sums in order.
-__global__ __launch_bounds__(256) void grad_join_kernel(GradPlan p, SumArgs a) {
-  __shared__ float sums[256][8];
-  const uint32_t piece = blockIdx.x / p.strips;
-  const int strip = (int)(blockIdx.x - piece * p.strips), group = threadIdx.x >> p.shift, groups = 256 >> p.shift;
-  const int lane = threadIdx.x & ((1 << p.shift) - 1), c = (strip << (p.shift + 3)) + lane * 8;
-  const uint32_t n = a.total[MAX_DIGITS];
-  const size_t first = (size_t)piece * p.piece, next = first + p.piece;
-  if (next >= n) return;
-  const uint32_t v = a.keys[next - 1];
-  if (a.keys[next] != v || (a.keys[first] == v && first > 0 && a.keys[first - 1] == v)) return;
-  uint32_t lo = (uint32_t)next, hi = n - 1;  // the last position of the run
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo + 1) / 2;
-    if (a.keys[mid] == v) lo = mid;
-    else hi = mid - 1;
+  if (came || far) {
+    part(came ? 0 : 1);
+    return;
   }
-  const uint32_t last = lo / p.piece, count = last - piece, per = (count + groups - 1) / groups;
-  float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  const uint32_t from = piece + 1 + group * per, to = from + per < last + 1 ? from + per : last + 1;
-  auto add = [&](uint32_t i, int which) {
-    float x[8];
-    OpRaw<float> o;
-    o.load(a.part + ((size_t)i * 2 + which) * a.part_ld + c, 8);
-    o.get(x);
+  if (goes) {  // into the next piece
+    uint32_t stop = end;
+    if constexpr (FULL) {
+      const uint64_t other = __ballot(next_key != cur || end + lane >= n);
+      stop = other ? end + (uint32_t)__builtin_ctzll(other) : end + 64;
+    } else {
+      while (stop < n && a.keys[stop] == cur) ++stop;
+    }
+    for (i = end; i < stop; i += AHEAD) {
+      OpRaw<T> row[AHEAD];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc[k] += x[k];
-  };
-  if (c < a.width) {
-    if (group == 0) add(piece, 1);
-    uint32_t i = from;
-    for (; i + 8 <= to; i += 8) {
-      OpRaw<float> o[8];
+      for (uint32_t j = 0; j < AHEAD; ++j) {
+        const uint32_t at = i + j < stop ? i + j : stop - 1;
+        row[j].load(src + (FULL ? lane_of(next_pos, at - end) : a.pos[at]) * a.dout_ld, left);
+      }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j].load(a.part + (size_t)(i + j) * 2 * a.part_ld + c, 8);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (uint32_t j = 0; j < AHEAD; ++j) {
+        if (i + j >= stop) break;
         float x[8];
-        o[j].get(x);
+        row[j].get(x);
 #pragma unroll
         for (int k = 0; k < 8; ++k) acc[k] += x[k];
       }
     }
-    for (; i < to; ++i) add(i, 0);
   }
+  if (c < a.width) grad_put(a, cur, c, acc);
+}
+// The runs that reach past the next piece: the workgroup of the pieces they start in adds their parts, its groups of lanes in equal ranges of the pieces
+// in between, then the groups' sums by pairs. 16 pieces per workgroup; few have such a run.
+constexpr int JOIN_THREADS = 1024;
+__global__ __launch_bounds__(JOIN_THREADS) void grad_join_kernel(GradPlan p, SumArgs a) {
+  __shared__ __align__(16) float sums[JOIN_THREADS][8];
+  const uint32_t block = blockIdx.x / p.strips, P = p.piece;
+  const int strip = (int)(blockIdx.x - block * p.strips), group = threadIdx.x >> p.shift, groups = JOIN_THREADS >> p.shift;
+  const int lane = threadIdx.x & ((1 << p.shift) - 1), c = (strip << (p.shift + 3)) + lane * 8;
+  const uint32_t n = a.total[MAX_DIGITS];
+  uint32_t key = 0;
+  bool owner = false;
+  {
+    const size_t first = ((size_t)block * 16 + (threadIdx.x & 15)) * P, next = first + P;
+    if (next + P < n) {
+      key = a.keys[next - 1];
+      const uint32_t k0 = a.keys[first > 0 ? first - 1 : 0], k1 = a.keys[first], k2 = a.keys[next], k3 = a.keys[next + P];
+      owner = k2 == key && k3 == key && !(k1 == key && first > 0 && k0 == key);
+    }
+  }
+  for (uint32_t owners = (uint32_t)__ballot(owner) & 0xffffu; owners; owners &= owners - 1) {  // the same in every wavefront
+    const uint32_t at_owner = (uint32_t)__builtin_ctz(owners), piece = block * 16 + at_owner, next = (piece + 1) * P;
+    const uint32_t v = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)at_owner);
+    // the last position of the run: 64 probes at a time, each step leaves a 64th
+    uint32_t lo = next, span = n - next;
+    while (span > 1) {
+      const uint32_t step = (span + 63) / 64, at = (threadIdx.x & 63) * step;
+      const uint64_t in = __ballot(at < span && a.keys[lo + (at < span ? at : 0)] == v);
+      const uint32_t have = (uint32_t)__popcll(in);  // the first ones
+      lo += (have - 1) * step;
+      span = n - lo < step ? n - lo : step;
+    }
+    const uint32_t last = lo / P, count = last - piece, per = (count + groups - 1) / groups;
+    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t from = piece + 1 + group * per, to = from + per < last + 1 ? from + per : last + 1;
+    if (c < a.width) {
+      if (group == 0) {
+        OpRaw<float> o;
+        o.load(a.part + ((size_t)piece * 2 + 1) * a.part_ld + c, 8);
+        o.get(acc);
+      }
+      for (uint32_t i = from; i < to; i += 4) {
+        OpRaw<float> o[4];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) sums[threadIdx.x][k] = acc[k];
-  __syncthreads();
-  if (group != 0 || c >= a.width) return;
-  for (int g = 1; g < groups; ++g)
+        for (uint32_t j = 0; j < 4; ++j) o[j].load(a.part + (size_t)(i + j < to ? i + j : to - 1) * 2 * a.part_ld + c, 8);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc[k] += sums[(g << p.shift) + lane][k];
-  grad_put(a, v, c, acc);
+        for (uint32_t j = 0; j < 4; ++j) {
+          if (i + j >= to) break;
+          float x[8];
+          o[j].get(x);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) acc[k] += x[k];
+        }
+      }
+    }
+    f32x4 *mine = reinterpret_cast<f32x4 *>(sums[threadIdx.x]);
+    mine[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+    mine[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
+    for (int half = groups / 2; half > 0; half /= 2) {
+      __syncthreads();
+      if (group < half) {
+        const f32x4 *other = reinterpret_cast<const f32x4 *>(sums[threadIdx.x + (half << p.shift)]);
+        mine[0] += other[0];
+        mine[1] += other[1];
+      }
+    }
+    __syncthreads();
+    if (group == 0 && c < a.width) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] = sums[threadIdx.x][k];
+      grad_put(a, v, c, acc);
+    }
+    __syncthreads();
+  }
 }
 
 }  // namespace
@@ -397,6 +467,6 @@ hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout
   auto *sum = dout.f32 ? (p.shift == 6 ? grad_sum_kernel<float, true> : grad_sum_kernel<float, false>)
                        : (p.shift == 6 ? grad_sum_kernel<bf16_t, true> : grad_sum_kernel<bf16_t, false>);
   hipLaunchKernelGGL(sum, sums, b, 0, s, p, a);
-  if (p.pieces > 1) hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)((size_t)p.pieces * p.strips)), b, 0, s, p, a);
+  if (p.pieces > 2) hipLaunchKernelGGL(grad_join_kernel, dim3((p.pieces + 15) / 16 * (uint32_t)p.strips), dim3(JOIN_THREADS), 0, s, p, a);
   return hipGetLastError();
 }

@@ -11,7 +11,7 @@ struct GradPlan {
   int passes, bits;             // digits
   uint32_t n, vocab, tiles;
   int shift, strips;            // 2^shift lanes on a strip of columns, 8 each
-  uint32_t piece, pieces;       // sorted positions summed by one group of lanes, at most 62
+  uint32_t piece, pieces;       // sorted positions summed by one group of lanes, at most 60
   size_t keys[2], pos[2], hist, total, flags, part, bytes;
 };
 constexpr int MAX_DIGITS = 1024, SORT_ITEMS = 4;  // elements per thread of a tile of 256 threads
