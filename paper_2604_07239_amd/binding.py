@@ -2,6 +2,7 @@
 context's device; host buffers are numpy arrays."""
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -99,8 +100,8 @@ def lib():
         L.fade_checkpoint_weight_grad.argtypes = [vp, vp, sz, sz, vp, i, sz, sz, vp, sz, i, vp, sz]
         L.fade_join_grad_work.restype = sz
         L.fade_join_grad_work.argtypes = [sz, sz]
-        L.fade_join.argtypes = [vp, C.POINTER(JoinArgs)]
-        L.fade_join_grad.argtypes = [vp, C.POINTER(JoinArgs)]
+        L.fade_join.argtypes = [vp, vp]
+        L.fade_join_grad.argtypes = [vp, vp]
         L.fade_tap.restype = sz
         L.fade_tap.argtypes = [vp, C.c_int, vp, sz]
         L.fade_get_weights.argtypes = [vp, vp, sz]
@@ -132,8 +133,19 @@ def _dp(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16}
-_TOKENS = {"torch.uint8": TOKEN_U8, "torch.int32": TOKEN_I32, "torch.int64": TOKEN_I64}
+# fade_join_args, packed in one go: a call from Python costs what its argument handling costs (fields one by one: 14 us a call, 6 this way)
+_JOIN = struct.Struct("@3If2Q4I5P3P3Q2P2Q4P2P2Q3P3Q5PPQ")
+assert _JOIN.size == C.sizeof(JoinArgs)
+_NO_GRADS = (0,) * 17
+_TYPES, _TOKENS = {}, {}
+
+
+def _type_of(table, t):
+    if not table:  # torch is the caller's: its types are looked up when the first tensor comes
+        import torch
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+        _TOKENS.update({torch.uint8: TOKEN_U8, torch.int32: TOKEN_I32, torch.int64: TOKEN_I64})
+    return table.get(t.dtype)
 
 
 class Fade:
@@ -264,31 +276,35 @@ class Fade:
 
     def _rows(self, t, name, rows=None, width=None, f32=False):
         """(pointer, type, ld) of a matrix [rows][width] whose columns are neighbours."""
-        kind = _TYPES.get(str(t.dtype))
-        if kind is None or (f32 and kind != F32) or t.dim() != 2 or not t.is_cuda or t.device.index != self.cfg.device:
+        kind = _type_of(_TYPES, t)
+        shape = t.shape
+        if kind is None or (f32 and kind != F32) or len(shape) != 2 or t.get_device() != self.cfg.device:
             self._bad(f"{name}: a matrix of {'float32' if f32 else 'float32 or bfloat16'} on the context's device is needed")
-        if (rows is not None and t.shape[0] != rows) or (width is not None and t.shape[1] != width):
-            self._bad(f"{name}: shape {tuple(t.shape)} where [{rows}, {width}] is needed")
-        if t.shape[1] > 1 and t.stride(1) != 1:
+        n, w = shape
+        if (rows is not None and n != rows) or (width is not None and w != width):
+            self._bad(f"{name}: shape {tuple(shape)} where [{rows}, {width}] is needed")
+        ld, step = t.stride()
+        if step != 1 and w > 1:
             self._bad(f"{name}: neighbouring columns have to be neighbours in memory")
-        return t.data_ptr(), kind, (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        return t.data_ptr(), kind, ld if n > 1 else w
 
     def _vector(self, t, name, count):
         if t is None:
-            return None
-        if str(t.dtype) != "torch.float32" or not t.is_cuda or t.device.index != self.cfg.device or t.numel() != count or not t.is_contiguous():
+            return 0
+        if _type_of(_TYPES, t) != F32 or t.get_device() != self.cfg.device or t.numel() != count or not t.is_contiguous():
             self._bad(f"{name}: {count} contiguous float32 values on the context's device are needed")
         return t.data_ptr()
 
     def _bytes(self, t, name, least):
-        """Pointer to a buffer of at least `least` bytes."""
-        if not t.is_cuda or t.device.index != self.cfg.device or not t.is_contiguous() or t.numel() * t.element_size() < least:
+        """(pointer, size) of a buffer of at least `least` bytes."""
+        size = t.nbytes
+        if t.get_device() != self.cfg.device or not t.is_contiguous() or size < least:
             self._bad(f"{name}: a contiguous buffer of {least} bytes on the context's device is needed")
-        return t.data_ptr()
+        return t.data_ptr(), size
 
     def _tokens(self, t):
-        kind = _TOKENS.get(str(t.dtype))
-        if kind is None or not t.is_cuda or t.device.index != self.cfg.device or not t.is_contiguous():
+        kind = _type_of(_TOKENS, t)
+        if kind is None or t.get_device() != self.cfg.device or not t.is_contiguous():
             self._bad("tokens: contiguous uint8, int32 or int64 values on the context's device are needed")
         return t.data_ptr(), kind, t.numel()
 
@@ -308,7 +324,7 @@ class Fade:
         gp, _, gld = self._rows(grad, "grad", f32=True)
         vocab, width = grad.shape
         dp, dk, dld = self._rows(dout, "dout", n, width)
-        wp, wn = self._bytes(work, "work", 0), work.numel() * work.element_size()
+        wp, wn = self._bytes(work, "work", 0)
         self._chk(self.L.fade_embed_grad(self.h, tp, tk, n, dp, dk, dld, scale, gp, gld, vocab, width, int(accumulate), wp, wn))
 
     def checkpoint_nbytes(self, rows, width):
@@ -318,13 +334,14 @@ class Fade:
         """Writes the 8-bit checkpoint of x [rows][width] into keep (checkpoint_nbytes(rows, width) bytes)."""
         xp, xk, xld = self._rows(x, "x")
         rows, width = x.shape
-        self._chk(self.L.fade_checkpoint(self.h, xp, xk, xld, rows, width, self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, width))))
+        self._chk(self.L.fade_checkpoint(self.h, xp, xk, xld, rows, width, self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, width))[0]))
 
     def checkpoint_read(self, keep, out):
         """The values a checkpoint stands for into out [rows][width]."""
         op, ok, old = self._rows(out, "out")
         rows, width = out.shape
-        self._chk(self.L.fade_checkpoint_read(self.h, self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, width)), rows, width, op, ok, old))
+        kp, _ = self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, width))
+        self._chk(self.L.fade_checkpoint_read(self.h, kp, rows, width, op, ok, old))
 
     def checkpoint_weight_grad_work(self, rows, in_width, out_width):
         return self.L.fade_checkpoint_weight_grad_work(rows, in_width, out_width)
@@ -335,51 +352,52 @@ class Fade:
         rows, n = dy.shape
         gp, _, gld = self._rows(grad, "grad", None, n, f32=True)
         k = grad.shape[0]
-        kp, wp = self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, k)), self._bytes(work, "work", 0)
-        self._chk(self.L.fade_checkpoint_weight_grad(self.h, kp, rows, k, dp, dk, dld, n, gp, gld, int(accumulate), wp, work.numel() * work.element_size()))
+        kp, _ = self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, k))
+        wp, wn = self._bytes(work, "work", 0)
+        self._chk(self.L.fade_checkpoint_weight_grad(self.h, kp, rows, k, dp, dk, dld, n, gp, gld, int(accumulate), wp, wn))
 
-    def _join_args(self, rows, width, stream, branch, norm_u, norm_n, eps, lam, params, matrices, keeps):
-        """matrices: (name, tensor, whether it is one of the stream's); stream, branch: element types, None where nothing says"""
+    def _join_side(self, tensors, rows, width):
+        """One element type and the pointers and strides of the matrices of one side of a join (the stream's or the branch's)."""
+        side, at, ld = None, [], []
+        for name, t in tensors:
+            if t is None:
+                at.append(0)
+                ld.append(0)
+                continue
+            p, kind, d = self._rows(t, name, rows, width)
+            if side is None:
+                side = kind
+            elif kind != side:
+                self._bad(f"{name}: another type than the other matrices of its side")
+            at.append(p)
+            ld.append(d)
+        return side, at, ld
+
+    def _join_model(self, width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n):
         if norm_u not in NORMS or norm_n not in NORMS:
             self._bad(f"norm: one of {', '.join(NORMS)} is needed")
-        a = JoinArgs(struct_size=C.sizeof(JoinArgs), norm_u=NORMS[norm_u], norm_n=NORMS[norm_n], eps=eps, rows=rows, width=width)
-        kinds = [stream, branch]
-        for name, t, of_stream in matrices:
-            if t is None:
-                continue
-            p, kind, ld = self._rows(t, name, rows, width)
-            side = 0 if of_stream else 1
-            if kinds[side] is None:
-                kinds[side] = kind
-            elif kinds[side] != kind:
-                self._bad(f"{name}: another type than the {'stream' if of_stream else 'branch'}'s other matrices")
-            setattr(a, name, p)
-            setattr(a, name + "_ld", ld)
-        # an operand that nobody gives has any type that goes with the other's
-        a.stream_type = kinds[0] if kinds[0] is not None else (kinds[1] or F32)
-        a.branch_type = kinds[1] if kinds[1] is not None else a.stream_type
+        count = 0
         if lam is not None:
-            a.lam_count = lam.numel()
-            if a.lam_count not in (1, width):
+            count = lam.numel()
+            if count not in (1, width):
                 self._bad(f"lam: 1 or {width} values are needed")
-            a.lam = self._vector(lam, "lam", a.lam_count)
-        for name, t in params:
-            if t is not None:
-                setattr(a, name, self._vector(t, name, a.lam_count if name == "d_lam" else width))
-        for name, t in keeps:
-            if t is not None:
-                setattr(a, name, self._bytes(t, name, self.L.fade_checkpoint_nbytes(rows, width)))
-        return a
+        v = self._vector
+        return count, (v(lam, "lam", count), v(gamma_u, "gamma_u", width), v(beta_u, "beta_u", width), v(gamma_n, "gamma_n", width), v(beta_n, "beta_n", width))
+
+    def _join_keeps(self, rows, width, *keeps):
+        least = self.L.fade_checkpoint_nbytes(rows, width) if any(t is not None for t in keeps) else 0
+        return [0 if t is None else self._bytes(t, "keep", least)[0] for t in keeps]
 
     def join(self, h, n=None, *, r, u, g=None, lam=None, norm_u="layer", norm_n="layer", gamma_u=None, beta_u=None, gamma_n=None, beta_n=None, eps=0.0,
              keep_r=None, keep_u=None, keep_g=None, keep_n=None):
         """h = lam * r + sigma(g) * norm_u(u) and n = norm_n(h), and 8-bit checkpoints of r, u, g and n where buffers are given."""
         rows, width = r.shape
-        a = self._join_args(rows, width, None, None, norm_u, norm_n, eps, lam,
-                            (("gamma_u", gamma_u), ("beta_u", beta_u), ("gamma_n", gamma_n), ("beta_n", beta_n)),
-                            (("r", r, True), ("h", h, True), ("u", u, False), ("g", g, False), ("n", n, False)),
-                            (("keep_r", keep_r), ("keep_u", keep_u), ("keep_g", keep_g), ("keep_n", keep_n)))
-        self._chk(self.L.fade_join(self.h, C.byref(a)))
+        stream, (rp, hp), (rl, hl) = self._join_side((("r", r), ("h", h)), rows, width)
+        branch, (up, gp, np_), (ul, gl, nl) = self._join_side((("u", u), ("g", g), ("n", n)), rows, width)
+        count, params = self._join_model(width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n)
+        a = _JOIN.pack(_JOIN.size, NORMS[norm_u], NORMS[norm_n], eps, rows, width, stream, branch, count, 0, *params, rp, up, gp, rl, ul, gl, hp, np_, hl, nl,
+                       *self._join_keeps(rows, width, keep_r, keep_u, keep_g, keep_n), *_NO_GRADS)
+        self._chk(self.L.fade_join(self.h, a))
 
     def join_grad_work(self, rows, width):
         return self.L.fade_join_grad_work(rows, width)
@@ -392,15 +410,17 @@ class Fade:
         if like is None:
             self._bad("neither dh nor dn")
         rows, width = like.shape
-        a = self._join_args(rows, width, None, None, norm_u, norm_n, eps, lam,
-                            (("gamma_u", gamma_u), ("beta_u", beta_u), ("gamma_n", gamma_n), ("beta_n", beta_n), ("d_lam", d_lam), ("d_gamma_u", d_gamma_u),
-                             ("d_beta_u", d_beta_u), ("d_gamma_n", d_gamma_n), ("d_beta_n", d_beta_n)),
-                            (("r", r, True), ("dh", dh, True), ("dr", dr, True), ("u", u, False), ("g", g, False), ("dn", dn, False), ("du", du, False),
-                             ("dg", dg, False)),
-                            (("keep_r", keep_r), ("keep_u", keep_u), ("keep_g", keep_g)))
-        a.accumulate = int(accumulate)
-        a.work, a.work_bytes = self._bytes(work, "work", 0), work.numel() * work.element_size()
-        self._chk(self.L.fade_join_grad(self.h, C.byref(a)))
+        stream, (rp, dhp, drp), (rl, dhl, drl) = self._join_side((("r", r), ("dh", dh), ("dr", dr)), rows, width)
+        branch, (up, gp, dnp, dup, dgp), (ul, gl, dnl, dul, dgl) = self._join_side((("u", u), ("g", g), ("dn", dn), ("du", du), ("dg", dg)), rows, width)
+        # a side that nobody gives has any type that goes with the other's
+        stream = stream if stream is not None else branch
+        branch = branch if branch is not None else stream
+        count, params = self._join_model(width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n)
+        v = self._vector
+        d = (v(d_lam, "d_lam", count), v(d_gamma_u, "d_gamma_u", width), v(d_beta_u, "d_beta_u", width), v(d_gamma_n, "d_gamma_n", width), v(d_beta_n, "d_beta_n", width))
+        a = _JOIN.pack(_JOIN.size, NORMS[norm_u], NORMS[norm_n], eps, rows, width, stream, branch, count, int(accumulate), *params, rp, up, gp, rl, ul, gl, 0, 0, 0, 0,
+                       *self._join_keeps(rows, width, keep_r, keep_u, keep_g, None), dhp, dnp, dhl, dnl, drp, dup, dgp, drl, dul, dgl, *d, *self._bytes(work, "work", 0))
+        self._chk(self.L.fade_join_grad(self.h, a))
 
     # -- profiling -------------------------------------------------------------------------------
     def profile(self, enable):
