@@ -178,6 +178,82 @@ __global__ __launch_bounds__(256) void sort_place_kernel(OpTokens t, GradPlan p,
     }
 }
 
+// The sort in one launch, for up to 16384 tokens: every workgroup reads all of them, keeps those of its own range of the vocabulary, and knows how many
+// lie in front of the range without asking another. Its wavefronts take consecutive parts of the tokens, 64 at a time, STEPS times; what each has
+// counted of a token in front gives the places. They are taken in LDS, and the range leaves in order: half of a text's tokens are in the first range,
+// and one compute unit's scattered stores of them took 30 us. The radix passes above are six launches of some four microseconds each there.
+template <int STEPS>
+__global__ __launch_bounds__(1024) void sort_ranges_kernel(OpTokens t, GradPlan p, uint32_t *total, uint32_t *keys_out, uint32_t *pos_out, uint8_t *flags) {
+  __shared__ uint32_t count[16][RANGE_TOKENS];  // per wavefront, then where its first position of the token goes
+  __shared__ uint32_t front[16], scans[16], total_here[1];
+  extern __shared__ uint32_t sorted[];  // [n]: position and, above 16 bits, token of the range
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t low = blockIdx.x * p.range, span = p.vocab - low < p.range ? p.vocab - low : p.range;
+  for (uint32_t d = tid; d < 16 * RANGE_TOKENS; d += 1024) count[d / RANGE_TOKENS][d % RANGE_TOKENS] = 0;
+  uint32_t key[STEPS], rank[STEPS], below_range = 0;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const uint32_t at = (uint32_t)(wave * STEPS + i) * 64 + lane;
+    key[i] = at < p.n ? token_at(t, at, p.vocab) : NO_TOKEN;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    below_range += key[i] < low ? 1 : 0;
+    const uint32_t d = key[i] - low;
+    const bool in = key[i] >= low && d < span;  // NO_TOKEN is past every range
+    uint64_t same = __ballot(in);
+    rank[i] = NO_TOKEN;
+    if (!same) continue;
+    for (int b = 0; b < p.range_bits; ++b) {
+      const bool one = (d >> b) & 1;
+      const uint64_t m = __ballot(one);
+      same &= one ? m : ~m;
+    }
+    const uint64_t before = same & (((uint64_t)1 << lane) - 1);
+    if (in) rank[i] = count[wave][d] + (uint32_t)__popcll(before);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (in && before == 0) count[wave][d] += (uint32_t)__popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  below_range = fade_lanes_sum(below_range);
+  if (lane == 0) front[wave] = below_range;
+  __syncthreads();
+  // a thread per token: its positions, the tokens in front, and the range's start
+  uint32_t mine = 0, start = 0;
+  if (tid < RANGE_TOKENS)
+    for (int w = 0; w < 16; ++w) mine += count[w][tid];
+  const uint32_t upto = fade_lanes_scan(mine);
+  if (lane == 63) scans[wave] = upto;
+  __syncthreads();
+  for (int w = 0; w < 16; ++w) start += front[w];
+  const uint32_t first = start;
+  start = 0;  // from here on within the range
+  for (int w = 0; w < wave; ++w) start += scans[w];
+  start += upto - mine;
+  if (tid < RANGE_TOKENS) {
+    if (tid < (int)span) flags[low + tid] = mine != 0;
+    if (tid == RANGE_TOKENS - 1) total_here[0] = start + mine;
+    for (int w = 0; w < 16; ++w) {
+      const uint32_t c = count[w][tid];
+      count[w][tid] = start;
+      start += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i)
+    if (rank[i] != NO_TOKEN) sorted[count[wave][key[i] - low] + rank[i]] = (uint32_t)(wave * STEPS + i) * 64 + lane | (key[i] - low) << 16;
+  __syncthreads();
+  const uint32_t have = total_here[0];
+  if (tid == 0 && blockIdx.x == gridDim.x - 1) total[MAX_DIGITS] = first + have;
+  for (uint32_t i = tid; i < have; i += 1024) {
+    const uint32_t v = sorted[i];
+    keys_out[first + i] = low + (v >> 16);
+    pos_out[first + i] = v & 0xffffu;
+  }
+}
+
 // ---------------------------------------------------------------------------------------------------
 // The sums
 // ---------------------------------------------------------------------------------------------------
@@ -185,6 +261,7 @@ struct SumArgs {
   const uint32_t *keys, *pos, *total;
   const uint8_t *flags;  // tokens that occur
   uint32_t clears;       // workgroups that write the rows of the others
+  uint32_t *ends;        // of a token whose run reaches past the next piece: the piece it ends in
   const void *dout;
   size_t dout_ld;
   float scale;
@@ -192,6 +269,7 @@ struct SumArgs {
   size_t grad_ld;
   float *part;   // [pieces][2][part_ld]: a run that came from the piece in front; one that starts here and goes on
   int width, part_ld;
+  uint32_t share;  // pieces per workgroup of the join, at most 16
   bool accumulate;
 };
 __device__ __forceinline__ void grad_put(const SumArgs &a, uint32_t v, int c, float x[8]) {
@@ -225,7 +303,7 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
         if (!(absent >> (r + mine) & 1)) continue;
         float *dst = a.grad + (size_t)(v0 + r + mine) * a.grad_ld;
         int c = first;
-        for (; c + 4 <= a.width; c += lanes * 4) __builtin_nontemporal_store(zero, reinterpret_cast<op_f32x4 *>(dst + c));
+        for (; c + 4 <= a.width; c += lanes * 4) *reinterpret_cast<op_f32x4 *>(dst + c) = zero;
         for (int k = c; k < a.width && k < c + 4; ++k) dst[k] = 0.0f;
       }
     }
@@ -260,7 +338,8 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
   const bool far = goes && end + P < n && far_behind == last_key;                   // nor in the next piece
   const bool from_far = came && begin > P && far_before == cur;                     // the first run does not start in the piece in front
   float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  auto part = [&](int which) {
+  auto part = [&](int which, bool ended) {
+    if (ended && c == 0) a.ends[cur] = piece;
     if (c >= a.width) return;
     OpRaw<float> o;
     o.put(acc);
@@ -294,7 +373,7 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
     for (uint32_t j = 0; j < AHEAD; ++j) {
       if (i + j >= end) break;
       if (key[j] != cur) {
-        if (came) part(0);
+        if (came) part(0, true);
         else if (c < a.width) grad_put(a, cur, c, acc);
         cur = key[j];
         came = false;
@@ -308,7 +387,7 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
     }
   }
   if (came || far) {
-    part(came ? 0 : 1);
+    part(came ? 0 : 1, came && !goes);
     return;
   }
   if (goes) {  // into the next piece
@@ -339,37 +418,27 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
   if (c < a.width) grad_put(a, cur, c, acc);
 }
 // The runs that reach past the next piece: the workgroup of the pieces they start in adds their parts, its groups of lanes in equal ranges of the pieces
-// in between, then the groups' sums by pairs. 16 pieces per workgroup; few have such a run.
-constexpr int JOIN_THREADS = 1024;
-__global__ __launch_bounds__(JOIN_THREADS) void grad_join_kernel(GradPlan p, SumArgs a) {
-  __shared__ __align__(16) float sums[JOIN_THREADS][8];
+// in between, then the groups' sums by pairs. A few pieces per workgroup; hardly any has such a run.
+template <int THREADS> __global__ __launch_bounds__(THREADS) void grad_join_kernel(GradPlan p, SumArgs a) {
+  __shared__ __align__(16) float sums[THREADS][8];
   const uint32_t block = blockIdx.x / p.strips, P = p.piece;
-  const int strip = (int)(blockIdx.x - block * p.strips), group = threadIdx.x >> p.shift, groups = JOIN_THREADS >> p.shift;
+  const int strip = (int)(blockIdx.x - block * p.strips), group = threadIdx.x >> p.shift, groups = THREADS >> p.shift;
   const int lane = threadIdx.x & ((1 << p.shift) - 1), c = (strip << (p.shift + 3)) + lane * 8;
   const uint32_t n = a.total[MAX_DIGITS];
   uint32_t key = 0;
   bool owner = false;
   {
-    const size_t first = ((size_t)block * 16 + (threadIdx.x & 15)) * P, next = first + P;
-    if (next + P < n) {
+    const size_t first = ((size_t)block * a.share + (threadIdx.x & 15)) * P, next = first + P;
+    if ((threadIdx.x & 15) < a.share && next + P < n) {
       key = a.keys[next - 1];
       const uint32_t k0 = a.keys[first > 0 ? first - 1 : 0], k1 = a.keys[first], k2 = a.keys[next], k3 = a.keys[next + P];
       owner = k2 == key && k3 == key && !(k1 == key && first > 0 && k0 == key);
     }
   }
   for (uint32_t owners = (uint32_t)__ballot(owner) & 0xffffu; owners; owners &= owners - 1) {  // the same in every wavefront
-    const uint32_t at_owner = (uint32_t)__builtin_ctz(owners), piece = block * 16 + at_owner, next = (piece + 1) * P;
+    const uint32_t at_owner = (uint32_t)__builtin_ctz(owners), piece = block * a.share + at_owner;
     const uint32_t v = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)at_owner);
-    // the last position of the run: 64 probes at a time, each step leaves a 64th
-    uint32_t lo = next, span = n - next;
-    while (span > 1) {
-      const uint32_t step = (span + 63) / 64, at = (threadIdx.x & 63) * step;
-      const uint64_t in = __ballot(at < span && a.keys[lo + (at < span ? at : 0)] == v);
-      const uint32_t have = (uint32_t)__popcll(in);  // the first ones
-      lo += (have - 1) * step;
-      span = n - lo < step ? n - lo : step;
-    }
-    const uint32_t last = lo / P, count = last - piece, per = (count + groups - 1) / groups;
+    const uint32_t last = a.ends[v], count = last - piece, per = (count + groups - 1) / groups;
     float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     const uint32_t from = piece + 1 + group * per, to = from + per < last + 1 ? from + per : last + 1;
     if (c < a.width) {
@@ -448,8 +517,17 @@ hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout
   uint8_t *flags = w + p.flags;
   const dim3 tiles(p.tiles), scans(((1u << p.bits) + 3) / 4), b(256);
   if (n == 0 && accumulate) return hipSuccess;
-  hipLaunchKernelGGL(sort_count_kernel<true>, tiles, b, 0, s, t, p, nullptr, nullptr, hist, flags, 0);
-  if (n) {
+  if (p.range) {
+    const dim3 ranges((p.vocab + p.range - 1) / p.range);
+    auto *f = n <= 4096 ? sort_ranges_kernel<4> : n <= 8192 ? sort_ranges_kernel<8> : sort_ranges_kernel<16>;
+    const size_t lds = (4 * n + 15) & ~(size_t)15;
+    if (lds > 32 * 1024) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(f, ranges, dim3(1024), lds, s, t, p, total, k0, p0, flags);
+  } else {
+    hipLaunchKernelGGL(sort_count_kernel<true>, tiles, b, 0, s, t, p, nullptr, nullptr, hist, flags, 0);
     hipLaunchKernelGGL(sort_scan_kernel, scans, b, 0, s, p, hist, total);
     if (p.passes == 1) {
       hipLaunchKernelGGL((sort_place_kernel<true, true>), tiles, b, 0, s, t, p, nullptr, nullptr, hist, total, k0, p0, flags, 0);
@@ -461,12 +539,16 @@ hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout
     }
   }
   const uint32_t groups = 256 >> p.shift, rows = (uint32_t)((vocab + groups - 1) / groups), clears = accumulate ? 0 : rows < 256 ? rows : 256;
-  const SumArgs a{k0, p0, total, flags, clears, dout.p, dout.ld, scale, grad, grad_ld, reinterpret_cast<float *>(w + p.part), (int)width, (int)((width + 7) & ~(size_t)7),
-                  accumulate};
+  const SumArgs a{k0, p0, total, flags, clears, words(p.ends), dout.p, dout.ld, scale, grad, grad_ld, reinterpret_cast<float *>(w + p.part), (int)width, (int)((width + 7) & ~(size_t)7),
+                  p.shift == 6 ? 4u : 16u, accumulate};
   const dim3 sums(clears + (uint32_t)(((size_t)p.pieces * p.strips + groups - 1) / groups));
   auto *sum = dout.f32 ? (p.shift == 6 ? grad_sum_kernel<float, true> : grad_sum_kernel<float, false>)
                        : (p.shift == 6 ? grad_sum_kernel<bf16_t, true> : grad_sum_kernel<bf16_t, false>);
   hipLaunchKernelGGL(sum, sums, b, 0, s, p, a);
-  if (p.pieces > 2) hipLaunchKernelGGL(grad_join_kernel, dim3((p.pieces + 15) / 16 * (uint32_t)p.strips), dim3(JOIN_THREADS), 0, s, p, a);
+  const dim3 joins((p.pieces + a.share - 1) / a.share * (uint32_t)p.strips);
+  if (p.pieces > 2) {
+    if (p.shift == 6) hipLaunchKernelGGL(grad_join_kernel<512>, joins, dim3(512), 0, s, p, a);
+    else hipLaunchKernelGGL(grad_join_kernel<1024>, joins, dim3(1024), 0, s, p, a);
+  }
   return hipGetLastError();
 }

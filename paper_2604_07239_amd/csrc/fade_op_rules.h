@@ -12,9 +12,12 @@ struct GradPlan {
   uint32_t n, vocab, tiles;
   int shift, strips;            // 2^shift lanes on a strip of columns, 8 each
   uint32_t piece, pieces;       // sorted positions summed by one group of lanes, at most 60
-  size_t keys[2], pos[2], hist, total, flags, part, bytes;
+  uint32_t range;               // one-launch sort: tokens of the vocabulary per workgroup; 0: radix passes
+  int range_bits;
+  size_t keys[2], pos[2], hist, total, flags, ends, part, bytes;
 };
 constexpr int MAX_DIGITS = 1024, SORT_ITEMS = 4;  // elements per thread of a tile of 256 threads
+constexpr int RANGE_TOKENS = 256;              // of a workgroup of the one-launch sort, at most
 
 inline int lanes_shift(size_t width, int most) {  // lanes for a row of this width: the least power of two that covers it, at most 2^most
   int s = 2;
@@ -30,11 +33,18 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
   p.n = (uint32_t)n;
   p.vocab = (uint32_t)vocab;
   p.tiles = n ? (uint32_t)((n + 256 * SORT_ITEMS - 1) / (256 * SORT_ITEMS)) : 1;
+  // Every workgroup of the one-launch sort reads all the tokens, and the one with the frequent ones ranks most of them: up to 8192 of them by 512 workgroups, or
+  // 16384 where a range has so few tokens that ranking them takes few comparisons. One launch | radix passes, us: 4096 of 32000 5.6 | 17; 16384 of 256 10.8 | 14;
+  // 32768 of 65536 39 | 25.
+  p.range = (uint32_t)((vocab + 255) / 256);
+  if (p.range > RANGE_TOKENS) p.range = RANGE_TOKENS;
+  if (n > (p.range <= 16 ? 16384 : 8192) || n * ((vocab + p.range - 1) / p.range) > (size_t)1 << 22) p.range = 0;
+  while (((uint32_t)1 << p.range_bits) < p.range) ++p.range_bits;
   p.shift = lanes_shift(width, 6);
   p.strips = (int)((width + ((size_t)8 << p.shift) - 1) / ((size_t)8 << p.shift));
   // as many pieces as there are wavefronts for, but none so short that the partial sums at their borders cost more than the rows between
   const size_t want = n * p.strips >> (6 - p.shift);
-  p.piece = (uint32_t)(want >= (size_t)1 << 18 ? 60 : want >= (size_t)1 << 17 ? 32 : want >= (size_t)1 << 15 ? 16 : 8);
+  p.piece = (uint32_t)(want >= (size_t)1 << 18 ? 60 : want >= (size_t)1 << 16 ? 32 : want >= (size_t)1 << 15 ? 16 : 8);
   p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -49,6 +59,7 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
   p.hist = take((size_t)4 * p.tiles << p.bits);
   p.total = take(4 * (MAX_DIGITS + 4));  // the digits' counts, then how many positions have a token at all
   p.flags = take(vocab);
+  p.ends = take(4 * vocab);
   p.part = take((size_t)2 * p.pieces * 4 * ((width + 7) & ~(size_t)7));
   p.bytes = at;
   return p;

@@ -187,7 +187,9 @@ int main() {
         }
         WANT(p.hist >= at && p.total >= p.hist + ((size_t)4 * p.tiles << p.bits));
         WANT(p.flags >= p.total + 4 * (MAX_DIGITS + 1) && p.flags % 16 == 0);
-        WANT(p.part >= p.flags + (vocab + 15) / 16 * 16 && p.part % 16 == 0);
+        WANT(p.ends >= p.flags + (vocab + 15) / 16 * 16 && p.part >= p.ends + 4 * vocab && p.part % 16 == 0);
+        WANT(p.piece >= 1 && p.piece <= 60);
+        WANT(p.range == 0 || (n <= 16384 && p.range <= RANGE_TOKENS && (1u << p.range_bits) >= p.range));
         WANT(p.bytes >= p.part + (size_t)2 * p.pieces * 4 * ((width + 7) / 8 * 8));
       }
   for (size_t rows : {(size_t)0, (size_t)1, (size_t)64, (size_t)65, (size_t)1500, (size_t)16384, (size_t)100001, (size_t)0x7fffffff})
