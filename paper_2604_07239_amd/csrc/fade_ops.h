@@ -177,11 +177,8 @@ __device__ __forceinline__ uint2 op_keep_pack(const float x[8], uint32_t &e) {
   }
   return make_uint2(w[0], w[1]);
 }
-// As unsigned bytes they are 128 too large, which one instruction each converts. (unit * byte - 128 unit in one step would leave fp32's range at the largest
-// units.) An infinite unit gives NaNs.
-__device__ __forceinline__ void op_keep_unpack(uint2 q, float unit, float x[8]) {
-  q.x ^= 0x80808080u;
-  q.y ^= 0x80808080u;
+// A byte of a word is converted with its sign in one instruction (SDWA), then scaled. An infinite unit gives NaNs.
+__device__ __forceinline__ void op_keep_unpack(const uint2 q, float unit, float x[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = ((float)(((i < 4 ? q.x : q.y) >> ((i & 3) * 8)) & 0xffu) - 128.0f) * unit;
+  for (int i = 0; i < 8; ++i) x[i] = (float)(int8_t)((i < 4 ? q.x : q.y) >> ((i & 3) * 8)) * unit;
 }
