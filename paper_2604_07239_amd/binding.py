@@ -133,15 +133,16 @@ def _dp(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
-# fade_join_args, packed in one go: a call from Python costs what its argument handling costs (fields one by one: 14 us a call, 6 this way)
+# fade_join_args, packed in one go: a call from Python costs what its argument handling costs (fields one by one: 14 us a call)
 _JOIN = struct.Struct("@3If2Q4I5P3P3Q2P2Q4P2P2Q3P3Q5PPQ")
 assert _JOIN.size == C.sizeof(JoinArgs)
 _NO_GRADS = (0,) * 17
 _TYPES, _TOKENS = {}, {}
 
 
-def _type_of(table, t):
-    if not table:  # torch is the caller's: its types are looked up when the first tensor comes
+def _late_type(table, t):
+    """torch is the caller's: its types are looked up when the first tensor comes."""
+    if not _TYPES:
         import torch
         _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
         _TOKENS.update({torch.uint8: TOKEN_U8, torch.int32: TOKEN_I32, torch.int64: TOKEN_I64})
@@ -159,7 +160,7 @@ class Fade:
         if rc:
             raise FadeError(rc, "fade_create")
         self.h = h
-        self.B, self.T = cfg.B, cfg.T
+        self.B, self.T, self.device = cfg.B, cfg.T, cfg.device
 
     def _chk(self, rc):
         if rc:
@@ -274,39 +275,61 @@ class Fade:
     def _bad(self, what):
         raise FadeError(-1, what)
 
-    def _rows(self, t, name, rows=None, width=None, f32=False):
+    def _rows(self, t, name, rows=None, width=None):
         """(pointer, type, ld) of a matrix [rows][width] whose columns are neighbours."""
-        kind = _type_of(_TYPES, t)
-        shape = t.shape
-        if kind is None or (f32 and kind != F32) or len(shape) != 2 or t.get_device() != self.cfg.device:
-            self._bad(f"{name}: a matrix of {'float32' if f32 else 'float32 or bfloat16'} on the context's device is needed")
-        n, w = shape
+        kind = _TYPES.get(t.dtype)
+        if kind is None:
+            kind = _late_type(_TYPES, t)
+        if kind is None or t.dim() != 2 or t.get_device() != self.device:
+            self._bad(f"{name}: a matrix of float32 or bfloat16 on the context's device is needed")
+        n, w = t.shape
         if (rows is not None and n != rows) or (width is not None and w != width):
-            self._bad(f"{name}: shape {tuple(shape)} where [{rows}, {width}] is needed")
+            self._bad(f"{name}: shape {(n, w)} where [{rows}, {width}] is needed")
         ld, step = t.stride()
         if step != 1 and w > 1:
             self._bad(f"{name}: neighbouring columns have to be neighbours in memory")
         return t.data_ptr(), kind, ld if n > 1 else w
 
+    def _same(self, t, name, rows, width, kind):
+        """(pointer, ld) of a matrix of a known type, or of none."""
+        if t is None:
+            return 0, 0
+        p, k, ld = self._rows(t, name, rows, width)
+        if k != kind:
+            self._bad(f"{name}: another type than the other matrices of its side")
+        return p, ld
+
     def _vector(self, t, name, count):
         if t is None:
             return 0
-        if _type_of(_TYPES, t) != F32 or t.get_device() != self.cfg.device or t.numel() != count or not t.is_contiguous():
+        kind = _TYPES.get(t.dtype)
+        if kind is None:
+            kind = _late_type(_TYPES, t)
+        if kind != F32 or t.get_device() != self.device or t.numel() != count or not t.is_contiguous():
             self._bad(f"{name}: {count} contiguous float32 values on the context's device are needed")
         return t.data_ptr()
 
     def _bytes(self, t, name, least):
         """(pointer, size) of a buffer of at least `least` bytes."""
         size = t.nbytes
-        if t.get_device() != self.cfg.device or not t.is_contiguous() or size < least:
+        if t.get_device() != self.device or not t.is_contiguous() or size < least:
             self._bad(f"{name}: a contiguous buffer of {least} bytes on the context's device is needed")
         return t.data_ptr(), size
 
     def _tokens(self, t):
-        kind = _type_of(_TOKENS, t)
-        if kind is None or t.get_device() != self.cfg.device or not t.is_contiguous():
+        kind = _TOKENS.get(t.dtype)
+        if kind is None:
+            kind = _late_type(_TOKENS, t)
+        if kind is None or t.get_device() != self.device or not t.is_contiguous():
             self._bad("tokens: contiguous uint8, int32 or int64 values on the context's device are needed")
         return t.data_ptr(), kind, t.numel()
+
+    def _grad(self, t, width=None):
+        """(pointer, ld) of a gradient: a matrix of float32."""
+        p, kind, ld = self._rows(t, "grad", None, width)
+        if kind != F32:
+            self._bad("grad: float32 is needed")
+        return p, ld
 
     def embed(self, tokens, table, out, scale=1.0):
         """out[i] = scale * table[tokens[i]]; tokens outside the table give zeros."""
@@ -321,7 +344,7 @@ class Fade:
     def embed_grad(self, tokens, dout, grad, work, scale=1.0, accumulate=False):
         """grad[v] = scale * sum of dout[i] where tokens[i] == v, or that added to grad."""
         tp, tk, n = self._tokens(tokens)
-        gp, _, gld = self._rows(grad, "grad", f32=True)
+        gp, gld = self._grad(grad)
         vocab, width = grad.shape
         dp, dk, dld = self._rows(dout, "dout", n, width)
         wp, wn = self._bytes(work, "work", 0)
@@ -350,28 +373,11 @@ class Fade:
         """grad [in][out] = x^T dy from the checkpoint of x [rows][in] and dy [rows][out], or that added to grad."""
         dp, dk, dld = self._rows(dy, "dy")
         rows, n = dy.shape
-        gp, _, gld = self._rows(grad, "grad", None, n, f32=True)
+        gp, gld = self._grad(grad, n)
         k = grad.shape[0]
         kp, _ = self._bytes(keep, "keep", self.L.fade_checkpoint_nbytes(rows, k))
         wp, wn = self._bytes(work, "work", 0)
         self._chk(self.L.fade_checkpoint_weight_grad(self.h, kp, rows, k, dp, dk, dld, n, gp, gld, int(accumulate), wp, wn))
-
-    def _join_side(self, tensors, rows, width):
-        """One element type and the pointers and strides of the matrices of one side of a join (the stream's or the branch's)."""
-        side, at, ld = None, [], []
-        for name, t in tensors:
-            if t is None:
-                at.append(0)
-                ld.append(0)
-                continue
-            p, kind, d = self._rows(t, name, rows, width)
-            if side is None:
-                side = kind
-            elif kind != side:
-                self._bad(f"{name}: another type than the other matrices of its side")
-            at.append(p)
-            ld.append(d)
-        return side, at, ld
 
     def _join_model(self, width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n):
         if norm_u not in NORMS or norm_n not in NORMS:
@@ -379,24 +385,27 @@ class Fade:
         count = 0
         if lam is not None:
             count = lam.numel()
-            if count not in (1, width):
+            if count != 1 and count != width:
                 self._bad(f"lam: 1 or {width} values are needed")
         v = self._vector
         return count, (v(lam, "lam", count), v(gamma_u, "gamma_u", width), v(beta_u, "beta_u", width), v(gamma_n, "gamma_n", width), v(beta_n, "beta_n", width))
 
-    def _join_keeps(self, rows, width, *keeps):
-        least = self.L.fade_checkpoint_nbytes(rows, width) if any(t is not None for t in keeps) else 0
-        return [0 if t is None else self._bytes(t, "keep", least)[0] for t in keeps]
+    def _keep(self, t, rows, width):
+        return 0 if t is None else self._bytes(t, "keep", self.L.fade_checkpoint_nbytes(rows, width))[0]
 
     def join(self, h, n=None, *, r, u, g=None, lam=None, norm_u="layer", norm_n="layer", gamma_u=None, beta_u=None, gamma_n=None, beta_n=None, eps=0.0,
              keep_r=None, keep_u=None, keep_g=None, keep_n=None):
         """h = lam * r + sigma(g) * norm_u(u) and n = norm_n(h), and 8-bit checkpoints of r, u, g and n where buffers are given."""
+        rp, stream, rl = self._rows(r, "r")
         rows, width = r.shape
-        stream, (rp, hp), (rl, hl) = self._join_side((("r", r), ("h", h)), rows, width)
-        branch, (up, gp, np_), (ul, gl, nl) = self._join_side((("u", u), ("g", g), ("n", n)), rows, width)
+        hp, hl = self._same(h, "h", rows, width, stream)
+        up, branch, ul = self._rows(u, "u", rows, width)
+        gp, gl = self._same(g, "g", rows, width, branch)
+        np_, nl = self._same(n, "n", rows, width, branch)
         count, params = self._join_model(width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n)
+        k = self._keep
         a = _JOIN.pack(_JOIN.size, NORMS[norm_u], NORMS[norm_n], eps, rows, width, stream, branch, count, 0, *params, rp, up, gp, rl, ul, gl, hp, np_, hl, nl,
-                       *self._join_keeps(rows, width, keep_r, keep_u, keep_g, keep_n), *_NO_GRADS)
+                       k(keep_r, rows, width), k(keep_u, rows, width), k(keep_g, rows, width), k(keep_n, rows, width), *_NO_GRADS)
         self._chk(self.L.fade_join(self.h, a))
 
     def join_grad_work(self, rows, width):
@@ -410,16 +419,23 @@ class Fade:
         if like is None:
             self._bad("neither dh nor dn")
         rows, width = like.shape
-        stream, (rp, dhp, drp), (rl, dhl, drl) = self._join_side((("r", r), ("dh", dh), ("dr", dr)), rows, width)
-        branch, (up, gp, dnp, dup, dgp), (ul, gl, dnl, dul, dgl) = self._join_side((("u", u), ("g", g), ("dn", dn), ("du", du), ("dg", dg)), rows, width)
-        # a side that nobody gives has any type that goes with the other's
-        stream = stream if stream is not None else branch
-        branch = branch if branch is not None else stream
+        # the type of each side is that of the first matrix given; a side that nobody gives has any type that goes with the other's
+        first_s = r if r is not None else dh if dh is not None else dr
+        first_b = u if u is not None else dn if dn is not None else du if du is not None else g if g is not None else dg
+        branch = self._rows(first_b, "the branch's matrices", rows, width)[1] if first_b is not None else None
+        stream = self._rows(first_s, "the stream's matrices", rows, width)[1] if first_s is not None else branch
+        if branch is None:
+            branch = stream
+        m = self._same
+        (rp, rl), (dhp, dhl), (drp, drl) = m(r, "r", rows, width, stream), m(dh, "dh", rows, width, stream), m(dr, "dr", rows, width, stream)
+        (up, ul), (gp, gl), (dnp, dnl) = m(u, "u", rows, width, branch), m(g, "g", rows, width, branch), m(dn, "dn", rows, width, branch)
+        (dup, dul), (dgp, dgl) = m(du, "du", rows, width, branch), m(dg, "dg", rows, width, branch)
         count, params = self._join_model(width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n)
-        v = self._vector
-        d = (v(d_lam, "d_lam", count), v(d_gamma_u, "d_gamma_u", width), v(d_beta_u, "d_beta_u", width), v(d_gamma_n, "d_gamma_n", width), v(d_beta_n, "d_beta_n", width))
+        v, k = self._vector, self._keep
         a = _JOIN.pack(_JOIN.size, NORMS[norm_u], NORMS[norm_n], eps, rows, width, stream, branch, count, int(accumulate), *params, rp, up, gp, rl, ul, gl, 0, 0, 0, 0,
-                       *self._join_keeps(rows, width, keep_r, keep_u, keep_g, None), dhp, dnp, dhl, dnl, drp, dup, dgp, drl, dul, dgl, *d, *self._bytes(work, "work", 0))
+                       k(keep_r, rows, width), k(keep_u, rows, width), k(keep_g, rows, width), 0, dhp, dnp, dhl, dnl, drp, dup, dgp, drl, dul, dgl,
+                       v(d_lam, "d_lam", count), v(d_gamma_u, "d_gamma_u", width), v(d_beta_u, "d_beta_u", width), v(d_gamma_n, "d_gamma_n", width),
+                       v(d_beta_n, "d_beta_n", width), *self._bytes(work, "work", 0))
         self._chk(self.L.fade_join_grad(self.h, a))
 
     # -- profiling -------------------------------------------------------------------------------

@@ -545,7 +545,7 @@ template <typename F> hipError_t with_types(const JoinArgs &a, F &&f) {
 hipError_t fade_join_launch(const JoinArgs &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const JoinShape sh = join_shape(a.width);
-  const int need = (a.rows + sh.groups - 1) / sh.groups, blocks = need < 2048 ? need : 2048;
+  const int blocks = even_blocks(a.rows, sh.groups, 2048);
   return with_types(a, [&](auto st, auto br) {
     return with_lanes(sh.lanes, [&](auto l) {
       constexpr int L = decltype(l)::value;

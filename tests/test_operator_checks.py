@@ -241,7 +241,7 @@ class _Ctx:
     def __new__(cls):
         import paper_2604_07239_amd as fa
         g = fa.Fade.__new__(fa.Fade)
-        g.cfg, g.L, g.h = fa.make_config(16, 32, 16, 128), fa.lib(), None
+        g.cfg, g.L, g.h, g.device = fa.make_config(16, 32, 16, 128), fa.lib(), None, 0
         return g
 
 
