@@ -274,11 +274,12 @@ def _plain(s):
 
 
 def _context():
-    """A program keeps one context; these calls need no weights in it."""
+    """A program keeps one context, on the stream of its other work (1 is HIP's name for the default one, where torch works); these calls
+    need no weights in it."""
     global _ctx
     if _ctx is None:
         import paper_2604_07239_amd as fade
-        _ctx = fade.Fade(fade.make_config(16, 32, 16, 128, dtype=fade.F32))
+        _ctx = fade.Fade(fade.make_config(16, 32, 16, 128, dtype=fade.F32, hip_stream=1))
     return _ctx
 
 
