@@ -294,12 +294,12 @@ __device__ __forceinline__ void grad_put(const SumArgs &a, uint32_t v, int c, fl
 // share the chip.
 template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum_kernel(GradPlan p, SumArgs a) {
   const uint32_t lane = threadIdx.x & 63;
-  if (blockIdx.x < a.clears) {  // 64 rows of the table per wavefront and turn
+  if (blockIdx.x < a.clears) {  // p.clear_rows rows of the table per wavefront and turn
     const op_f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     const int lanes = 1 << p.shift, first = (threadIdx.x & (lanes - 1)) * 4, rows = 64 >> p.shift, mine = (int)lane >> p.shift;
-    for (uint32_t v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; v0 < p.vocab; v0 += a.clears * 256) {
-      const uint64_t absent = __ballot(v0 + lane < p.vocab && !a.flags[v0 + lane]);
-      for (int r = 0; r < 64; r += rows) {
+    for (uint32_t v0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * p.clear_rows; v0 < p.vocab; v0 += a.clears * 4 * p.clear_rows) {
+      const uint64_t absent = __ballot(lane < p.clear_rows && v0 + lane < p.vocab && !a.flags[v0 + lane]);
+      for (int r = 0; r < (int)p.clear_rows; r += rows) {
         if (!(absent >> (r + mine) & 1)) continue;
         float *dst = a.grad + (size_t)(v0 + r + mine) * a.grad_ld;
         int c = first;
@@ -538,9 +538,9 @@ hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout
       hipLaunchKernelGGL((sort_place_kernel<false, true>), tiles, b, 0, s, t, p, k1, p1, hist, total, k0, p0, flags, p.bits);
     }
   }
-  const uint32_t groups = 256 >> p.shift, rows = (uint32_t)((vocab + groups - 1) / groups), clears = accumulate ? 0 : rows < 256 ? rows : 256;
+  const uint32_t groups = 256 >> p.shift, turns = (uint32_t)((vocab + 4 * p.clear_rows - 1) / (4 * p.clear_rows)), clears = accumulate ? 0 : turns < 512 ? turns : 512;
   const SumArgs a{k0, p0, total, flags, clears, words(p.ends), dout.p, dout.ld, scale, grad, grad_ld, reinterpret_cast<float *>(w + p.part), (int)width, (int)((width + 7) & ~(size_t)7),
-                  p.shift == 6 ? 4u : 16u, accumulate};
+                  p.share, accumulate};
   const dim3 sums(clears + (uint32_t)(((size_t)p.pieces * p.strips + groups - 1) / groups));
   auto *sum = dout.f32 ? (p.shift == 6 ? grad_sum_kernel<float, true> : grad_sum_kernel<float, false>)
                        : (p.shift == 6 ? grad_sum_kernel<bf16_t, true> : grad_sum_kernel<bf16_t, false>);

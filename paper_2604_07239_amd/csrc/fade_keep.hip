@@ -270,15 +270,20 @@ template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int n = n0 + (wn * TN + j) * 32 + (lane & 31);
+      const int n = n0 + (wn * TN + j) * 32 + (lane & 31), m = m0 + (wm * TM + i) * 32 + (lane >> 5) * 4;
       if (n >= g.N) continue;
+      float *dst = out + (size_t)m * g.out_ld + n;
+      const auto row = [](int e) { return (e >> 2) * 8 + (e & 3); };
+      if (g.add) {  // all of what is there at once
+        float old[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int m = m0 + (wm * TM + i) * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3);
-        if (m >= g.K) continue;
-        float *dst = out + (size_t)m * g.out_ld + n;
-        *dst = g.add ? *dst + acc[i][j][e] : acc[i][j][e];
+        for (int e = 0; e < 16; ++e) old[e] = m + row(e) < g.K ? dst[(size_t)row(e) * g.out_ld] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] += old[e];
       }
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (m + row(e) < g.K) dst[(size_t)row(e) * g.out_ld] = acc[i][j][e];
     }
 }
 // The ranges' sums, added in their order, V pieces of four values per thread: a gradient without gaps between its rows is one run of values; else a

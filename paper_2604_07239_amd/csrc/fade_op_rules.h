@@ -12,6 +12,8 @@ struct GradPlan {
   uint32_t n, vocab, tiles;
   int shift, strips;            // 2^shift lanes on a strip of columns, 8 each
   uint32_t piece, pieces;       // sorted positions summed by one group of lanes, at most 60
+  uint32_t share;               // pieces that a workgroup looks over for runs to join, at most 16
+  uint32_t clear_rows;          // of the gradient that a wavefront clears at a turn: a power of two, at least its groups of lanes
   uint32_t range;               // one-launch sort: tokens of the vocabulary per workgroup; 0: radix passes
   int range_bits;
   size_t keys[2], pos[2], hist, total, flags, ends, part, bytes;
@@ -41,11 +43,15 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
   if (n > (p.range <= 16 ? 16384 : 8192) || n * ((vocab + p.range - 1) / p.range) > (size_t)1 << 22) p.range = 0;
   while (((uint32_t)1 << p.range_bits) < p.range) ++p.range_bits;
   p.shift = lanes_shift(width, 6);
+  p.clear_rows = 64;
+  while (p.clear_rows > (64u >> p.shift) && vocab / p.clear_rows < 2048) p.clear_rows /= 2;
   p.strips = (int)((width + ((size_t)8 << p.shift) - 1) / ((size_t)8 << p.shift));
   // as many pieces as there are wavefronts for, but none so short that the partial sums at their borders cost more than the rows between
   const size_t want = n * p.strips >> (6 - p.shift);
   p.piece = (uint32_t)(want >= (size_t)1 << 18 ? 60 : want >= (size_t)1 << 16 ? 32 : want >= (size_t)1 << 15 ? 16 : 8);
   p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
+  const size_t looks = ((size_t)p.pieces * p.strips + 1023) / 1024;
+  p.share = looks > 16 ? 16 : looks < 1 ? 1 : (uint32_t)looks;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;

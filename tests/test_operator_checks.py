@@ -188,7 +188,8 @@ int main() {
         WANT(p.hist >= at && p.total >= p.hist + ((size_t)4 * p.tiles << p.bits));
         WANT(p.flags >= p.total + 4 * (MAX_DIGITS + 1) && p.flags % 16 == 0);
         WANT(p.ends >= p.flags + (vocab + 15) / 16 * 16 && p.part >= p.ends + 4 * vocab && p.part % 16 == 0);
-        WANT(p.piece >= 1 && p.piece <= 60);
+        WANT(p.piece >= 1 && p.piece <= 60 && p.share >= 1 && p.share <= 16);
+        WANT(p.clear_rows >= (64u >> p.shift) && p.clear_rows <= 64 && 64 % p.clear_rows == 0);
         WANT(p.range == 0 || (n <= 16384 && p.range <= RANGE_TOKENS && (1u << p.range_bits) >= p.range));
         WANT(p.bytes >= p.part + (size_t)2 * p.pieces * 4 * ((width + 7) / 8 * 8));
       }
