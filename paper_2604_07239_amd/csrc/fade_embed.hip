@@ -37,8 +37,9 @@ __global__ __launch_bounds__(256) void embed_kernel(OpTokens t, size_t n, const 
   for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < width; c += 8 << shift) {
     float x[8];
     OpRaw<TT> in;
-    if (v != NO_TOKEN) in.load(table + v * table_ld + c, width - c);
+    if (v != NO_TOKEN) in.load(table + v * table_ld + c, width - c, c);
     else in.zero();
+    in.fix(width - c, c);
     in.get(x);
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = v != NO_TOKEN ? x[k] * scale : 0.0f;
@@ -279,7 +280,8 @@ __device__ __forceinline__ void grad_put(const SumArgs &a, uint32_t v, int c, fl
   for (int k = 0; k < 8; ++k) x[k] *= a.scale;
   if (a.accumulate) {
     float old[8];
-    o.load(dst, a.width - c);
+    o.load(dst, a.width - c, c);
+    o.fix(a.width - c, c);
     o.get(old);
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] += old[k];
@@ -367,7 +369,7 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
     for (uint32_t j = 0; j < AHEAD; ++j) {
       const uint32_t at = i + j < end ? i + j : end - 1;
       key[j] = key_at(at);
-      row[j].load(src + (FULL ? lane_of(my_pos, at - begin) : a.pos[at]) * a.dout_ld, left);
+      row[j].load(src + (FULL ? lane_of(my_pos, at - begin) : a.pos[at]) * a.dout_ld, left, c);
     }
 #pragma unroll
     for (uint32_t j = 0; j < AHEAD; ++j) {
@@ -381,6 +383,7 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
         for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
       }
       float x[8];
+      row[j].fix(left, c);
       row[j].get(x);
 #pragma unroll
       for (int k = 0; k < 8; ++k) acc[k] += x[k];
@@ -403,12 +406,13 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
 #pragma unroll
       for (uint32_t j = 0; j < AHEAD; ++j) {
         const uint32_t at = i + j < stop ? i + j : stop - 1;
-        row[j].load(src + (FULL ? lane_of(next_pos, at - end) : a.pos[at]) * a.dout_ld, left);
+        row[j].load(src + (FULL ? lane_of(next_pos, at - end) : a.pos[at]) * a.dout_ld, left, c);
       }
 #pragma unroll
       for (uint32_t j = 0; j < AHEAD; ++j) {
         if (i + j >= stop) break;
         float x[8];
+        row[j].fix(left, c);
         row[j].get(x);
 #pragma unroll
         for (int k = 0; k < 8; ++k) acc[k] += x[k];

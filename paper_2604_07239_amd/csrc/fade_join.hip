@@ -113,7 +113,8 @@ __device__ __forceinline__ void param8(const float *p, float otherwise, int c, i
     for (int k = 0; k < 8; ++k) x[k] = k < left ? otherwise : 0.0f;
   } else {
     OpRaw<float> r;
-    r.load(p + c, left);
+    r.load(p + c, left, c);
+    r.fix(left, c);
     r.get(x);
   }
 }
@@ -148,6 +149,11 @@ template <int L> struct Lane {  // the same row for a whole wavefront is known t
   }
   __device__ __forceinline__ int wave() const { return L > 64 ? __builtin_amdgcn_readfirstlane(lane / 64) : 0; }
 };
+// 8 columns that have arrived, in their places (rows of whole pieces: there they are)
+template <bool WHOLE, int L, typename R> __device__ __forceinline__ R &arrived(R &raw, const Lane<L> &l) {
+  if constexpr (!WHOLE) raw.fix(l.left, l.c);
+  return raw;
+}
 // how many of 8 columns to move: all of them on rows of whole pieces
 template <bool WHOLE> __device__ __forceinline__ int op_left(int left) { return WHOLE ? 8 : left; }
 
@@ -178,9 +184,9 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
     if (row >= (size_t)a.rows) row = a.rows - 1;
     if (l.left > 0) {
       const int left = op_left<WHOLE>(l.left);
-      raw_r.load(static_cast<const TS *>(a.r) + row * a.r_ld + l.c, left);
-      raw_u.load(static_cast<const TB *>(a.u) + row * a.u_ld + l.c, left);
-      if (a.g) raw_g.load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c, left);
+      raw_r.load(static_cast<const TS *>(a.r) + row * a.r_ld + l.c, left, l.c);
+      raw_u.load(static_cast<const TB *>(a.u) + row * a.u_ld + l.c, left, l.c);
+      if (a.g) raw_g.load(static_cast<const TB *>(a.g) + row * a.g_ld + l.c, left, l.c);
     }
   };
   const bool has_n = a.n || a.keep_n;
@@ -188,7 +194,7 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
   uint32_t base = blockIdx.x * Sums::GROUPS;
   float x[8], mean_u, rstd_u;
   load(base + l.group);
-  raw_u.get(x);
+  arrived<WHOLE>(raw_u, l).get(x);
   {
     float v[2];
     rs.template part<WHOLE>(a.norm_u, x, l.left, v[0], v[1]);
@@ -199,7 +205,7 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
     const size_t row = base + l.group;
     const bool in = Sums::GROUPS == 1 || row < (size_t)a.rows;  // the workgroup's barriers are for all its rows
     float h[8], g[8], p[8], q[8];
-    raw_r.get(h); raw_g.get(g);
+    arrived<WHOLE>(raw_r, l).get(h); arrived<WHOLE>(raw_g, l).get(g);
     load(row + gridDim.x * Sums::GROUPS);
     if (a.keep_r) keep_row(a.keep_r, a.rows, a.width, row, in, h, l.c);
     if (a.keep_u) keep_row(a.keep_u, a.rows, a.width, row, in, x, l.c);
@@ -219,7 +225,7 @@ template <int L, typename TS, typename TB, bool WHOLE> __global__ __launch_bound
     }
     float v[4], mean, rstd;
     rs.template part<WHOLE>(norm_n, h, l.left, v[0], v[1]);
-    raw_u.get(x);
+    arrived<WHOLE>(raw_u, l).get(x);
     rs.template part<WHOLE>(a.norm_u, x, l.left, v[2], v[3]);
     rs.exchange(v);
     rs.whole(norm_n, v[0], v[1], a.eps, mean, rstd);
@@ -250,7 +256,8 @@ __host__ __device__ inline size_t part_width(int width) { return (size_t)((width
 template <typename T> struct SavedRaw {  // 8 columns of a saved operand: as it was
   OpRaw<T> v;
   __device__ __forceinline__ void zero() { v.zero(); }
-  __device__ __forceinline__ void load(const void *p, size_t ld, int, int, size_t row, int c, int left) { v.load(static_cast<const T *>(p) + row * ld + c, left); }
+  __device__ __forceinline__ void load(const void *p, size_t ld, int, int, size_t row, int c, int left) { v.load(static_cast<const T *>(p) + row * ld + c, left, c); }
+  __device__ __forceinline__ void fix(int left, int c) { v.fix(left, c); }
   __device__ __forceinline__ void get(float x[8]) const { v.get(x); }
 };
 struct SavedKeep {  // or from its checkpoint
@@ -263,6 +270,7 @@ struct SavedKeep {  // or from its checkpoint
     q = *reinterpret_cast<const uint2 *>(k + row * groups * 32 + c);
     e = k[(size_t)rows * groups * 32 + row * groups + (c >> 5)];
   }
+  __device__ __forceinline__ void fix(int, int) {}
   __device__ __forceinline__ void get(float x[8]) const { op_keep_unpack(q, op_keep_unit(e), x); }
 };
 
@@ -326,15 +334,15 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
       raw_r.load(src_r, a.r_ld, a.rows, a.width, row, l.c, left);
       raw_u.load(src_u, a.u_ld, a.rows, a.width, row, l.c, left);
       if (src_g) raw_g.load(src_g, a.g_ld, a.rows, a.width, row, l.c, left);
-      if (a.dh) raw_dh.load(static_cast<const TS *>(a.dh) + row * a.dh_ld + l.c, left);
-      if (a.dn) raw_dn.load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c, left);
+      if (a.dh) raw_dh.load(static_cast<const TS *>(a.dh) + row * a.dh_ld + l.c, left, l.c);
+      if (a.dn) raw_dn.load(static_cast<const TB *>(a.dn) + row * a.dn_ld + l.c, left, l.c);
     }
   };
   // Two exchanges a row: h's statistics with the sums of N_n's gradient, and the sums of N_u's with u's statistics of the next row.
   uint32_t base = blockIdx.x * GROUPS;
   float uhat[8], mean_u, rstd_u;
   load(base + l.group);
-  raw_u.get(uhat);
+  arrived<WHOLE>(raw_u, l).get(uhat);
   {
     float v[2];
     rs.template part<WHOLE>(a.norm_u, uhat, l.left, v[0], v[1]);
@@ -346,7 +354,7 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
     const bool in = GROUPS == 1 || row < (size_t)a.rows;
     // forward again: uhat, z, sigma(g), h
     float z[8], sg[8], r[8], t[8], e[8], w[8];
-    raw_r.get(r); raw_g.get(sg); raw_dh.get(t); raw_dn.get(e);
+    arrived<WHOLE>(raw_r, l).get(r); arrived<WHOLE>(raw_g, l).get(sg); arrived<WHOLE>(raw_dh, l).get(t); arrived<WHOLE>(raw_dn, l).get(e);
     load(row + gridDim.x * GROUPS);
     if (!in)  // a row that is not there adds zeros
 #pragma unroll
@@ -436,7 +444,7 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
       v[0] = wave_total<L>(v[0]);
       v[1] = wave_total<L>(v[1]);
     }
-    raw_u.get(x);
+    arrived<WHOLE>(raw_u, l).get(x);
     rs.template part<WHOLE>(a.norm_u, x, l.left, v[2], v[3]);
     rs.exchange(v);
     rs.whole(a.norm_u, v[2], v[3], a.eps, mean_u, rstd_u);
@@ -545,7 +553,7 @@ template <typename F> hipError_t with_types(const JoinArgs &a, F &&f) {
 hipError_t fade_join_launch(const JoinArgs &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const JoinShape sh = join_shape(a.width);
-  const int blocks = even_blocks(a.rows, sh.groups, 2048);
+  const int blocks = turn_blocks(a.rows, sh.groups, 2048);
   return with_types(a, [&](auto st, auto br) {
     return with_lanes(sh.lanes, [&](auto l) {
       constexpr int L = decltype(l)::value;

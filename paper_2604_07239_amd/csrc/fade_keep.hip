@@ -21,8 +21,9 @@ __global__ __launch_bounds__(256) void keep_kernel(const T *x, size_t ld, int wi
   for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < k.groups * 32; c += 8 << shift) {
     float v[8];
     OpRaw<T> in;
-    if (c < width) in.load(x + row * ld + c, width - c);
+    if (c < width) in.load(x + row * ld + c, width - c, c);
     else in.zero();
+    in.fix(width - c, c);
     in.get(v);
     uint32_t exp;
     const uint2 w = op_keep_pack(v, exp);
@@ -302,19 +303,19 @@ __global__ __launch_bounds__(256) void keep_grad_add_kernel(const float *part, i
   op_f32x4 s[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) s[k] = op_f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (left == 1024 * V) {  // all of them are there: loads of several ranges at once
-    constexpr int AHEAD = 8 / V;
+  constexpr int AHEAD = 8 / V;  // ranges whose loads are on their way together
+  if (at + (V - 1) * 1024 + 4 <= left) {
 #pragma unroll AHEAD
     for (int r = 0; r < ranges; ++r, src += count)
 #pragma unroll
       for (int k = 0; k < V; ++k) s[k] += *reinterpret_cast<const op_f32x4 *>(src + at + k * 1024);
-  } else {
+  } else {  // what does not exist is the block's first value again, and not stored
+#pragma unroll AHEAD
     for (int r = 0; r < ranges; ++r, src += count)
 #pragma unroll
       for (int k = 0; k < V; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (at + k * 1024 + i < left) s[k][i] += src[at + k * 1024 + i];
+        for (int i = 0; i < 4; ++i) s[k][i] += src[at + k * 1024 + i < left ? at + k * 1024 + i : 0];
   }
 #pragma unroll
   for (int k = 0; k < V; ++k) {

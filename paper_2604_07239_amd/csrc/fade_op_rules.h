@@ -115,15 +115,15 @@ inline JoinShape join_shape(size_t width) {
   while ((size_t)lanes * 8 < width) lanes *= 2;
   return {lanes, lanes >= 256 ? 1 : 256 / lanes};
 }
-// Workgroups for `rows` rows, at most `most`, all with as many turns as one another where that divides.
-inline int even_blocks(size_t rows, int groups, size_t most) {
-  const size_t need = (rows + groups - 1) / groups, turns = (need + most - 1) / most;
-  return turns ? (int)((need + turns - 1) / turns) : 0;
+// Workgroups that take rows in turn. The gradient's keep their columns' sums in registers over all their rows, so that they are two per compute unit (one of
+// 512 lanes and more). (As many fewer as give all of them equal turns: 1500 x 777 in 17.4 us instead of 14.4.)
+inline int turn_blocks(size_t rows, int groups, size_t most) {
+  const size_t need = (rows + groups - 1) / groups;
+  return (int)(need < most ? need : most);
 }
-// The gradient's workgroups keep their columns' sums in registers over all their rows, so that they are two per compute unit (one of 512 lanes and more).
 inline int grad_blocks(size_t rows, size_t width) {
   const JoinShape sh = join_shape(width);
-  return even_blocks(rows, sh.groups, sh.lanes >= 512 ? 256 : 512);
+  return turn_blocks(rows, sh.groups, sh.lanes >= 512 ? 256 : 512);
 }
 
 }  // namespace fade_op
