@@ -1,11 +1,11 @@
 // fade_embed.hip — embedding lookup with scaling, and its gradient by sorted tokens (gfx950).
 //
-// Forward: y[i] = scale * E[t_i], one pass over the output; bounded by its bytes.
+// Forward: y[i] = scale * E[t_i], one pass over the output, whose bytes bound it: 20011 tokens, width 1000, fp32 table, bf16 rows 15.4 us.
 // Gradient: G[v] = scale * sum of dy[i] over t_i = v. Atomics would add the rows of a token in any order, and the result would
 // differ from run to run; a decoder that repeats an encoder's training would leave it. So the positions are sorted by token first
-// (stable, hence ascending in every token's run), cut into pieces of equal length, and each piece is summed in order; a run that
-// crosses a piece's border leaves partial sums that a second kernel adds in order. The sort moves a few words a token, the sums
-// read dy once: from some hundred columns on the bytes of dy and G bound it.
+// (stable, hence ascending in every token's run) and cut into pieces of equal length, each summed in order by one group of lanes. The sort moves a
+// few words a token, the sums read dy once and write G once. 32768 tokens of 65536, width 2048, bf16: sort 25 us, sums 130 to 145 (671 MB at 4.6 to 5.2 TB/s: the
+// memory bounds them), long runs 9. 262144 bytes, width 64, fp32: sort 16, sums 14 (67 MB), long runs 13: there launches and dependent loads are most of it.
 #include "../../include/fade.h"
 #include "fade_op_rules.h"
 #include "fade_ops.h"
@@ -31,21 +31,21 @@ __device__ __forceinline__ uint32_t token_at(const OpTokens &t, size_t i, uint32
 template <typename TT, typename TO>
 __global__ __launch_bounds__(256) void embed_kernel(OpTokens t, size_t n, const TT *table, size_t table_ld, uint32_t vocab, int width, float scale,
                                                     TO *out, size_t out_ld, int shift) {
-  const size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
-  if (row >= n) return;
-  const uint32_t v = token_at(t, row, vocab);
-  for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < width; c += 8 << shift) {
-    float x[8];
-    OpRaw<TT> in;
-    if (v != NO_TOKEN) in.load(table + v * table_ld + c, width - c, c);
-    else in.zero();
-    in.fix(width - c, c);
-    in.get(x);
+  for (size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift); row < n; row += (size_t)gridDim.x * (256 >> shift)) {
+    const uint32_t v = token_at(t, row, vocab);
+    for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < width; c += 8 << shift) {
+      float x[8];
+      OpRaw<TT> in;
+      if (v != NO_TOKEN) in.load(table + v * table_ld + c, width - c, c);
+      else in.zero();
+      in.fix(width - c, c);
+      in.get(x);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = v != NO_TOKEN ? x[k] * scale : 0.0f;
-    OpRaw<TO> o;
-    o.put(x);
-    o.store(out + row * out_ld + c, width - c);
+      for (int k = 0; k < 8; ++k) x[k] = v != NO_TOKEN ? x[k] * scale : 0.0f;
+      OpRaw<TO> o;
+      o.put(x);
+      o.store(out + row * out_ld + c, width - c);
+    }
   }
 }
 
@@ -422,11 +422,12 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
   if (c < a.width) grad_put(a, cur, c, acc);
 }
 // The runs that reach past the next piece: the workgroup of the pieces they start in adds their parts, its groups of lanes in equal ranges of the pieces
-// in between, then the groups' sums by pairs. A few pieces per workgroup; hardly any has such a run.
-template <int THREADS> __global__ __launch_bounds__(THREADS) void grad_join_kernel(GradPlan p, SumArgs a) {
-  __shared__ __align__(16) float sums[THREADS][8];
+// in between. A few pieces per workgroup; hardly any has such a run.
+constexpr int JOIN_THREADS = 512;  // 262144 bytes: 13 us; 1024 15, 256 19
+__global__ __launch_bounds__(JOIN_THREADS) void grad_join_kernel(GradPlan p, SumArgs a) {
+  __shared__ __align__(16) float sums[JOIN_THREADS][8];
   const uint32_t block = blockIdx.x / p.strips, P = p.piece;
-  const int strip = (int)(blockIdx.x - block * p.strips), group = threadIdx.x >> p.shift, groups = THREADS >> p.shift;
+  const int strip = (int)(blockIdx.x - block * p.strips), group = threadIdx.x >> p.shift, groups = JOIN_THREADS >> p.shift;
   const int lane = threadIdx.x & ((1 << p.shift) - 1), c = (strip << (p.shift + 3)) + lane * 8;
   const uint32_t n = a.total[MAX_DIGITS];
   uint32_t key = 0;
@@ -465,21 +466,23 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void grad_join_kern
         }
       }
     }
+    // groups of one wavefront by exchanges, widest first, then the wavefronts in order
+    const auto plus = [](float a, float b) { return a + b; };
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (p.shift <= 5) acc[k] = fade_level<32>(acc[k], plus);
+      if (p.shift <= 4) acc[k] = fade_level<16>(acc[k], plus);
+      if (p.shift <= 3) acc[k] = fade_level<8>(acc[k], plus);
+      if (p.shift <= 2) acc[k] = fade_level<4>(acc[k], plus);
+    }
     f32x4 *mine = reinterpret_cast<f32x4 *>(sums[threadIdx.x]);
     mine[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
     mine[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
-    for (int half = groups / 2; half > 0; half /= 2) {
-      __syncthreads();
-      if (group < half) {
-        const f32x4 *other = reinterpret_cast<const f32x4 *>(sums[threadIdx.x + (half << p.shift)]);
-        mine[0] += other[0];
-        mine[1] += other[1];
-      }
-    }
     __syncthreads();
     if (group == 0 && c < a.width) {
+      for (int w = 1; w < JOIN_THREADS / 64; ++w)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] = sums[threadIdx.x][k];
+        for (int k = 0; k < 8; ++k) acc[k] += sums[w * 64 + lane][k];
       grad_put(a, v, c, acc);
     }
     __syncthreads();
@@ -490,7 +493,7 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void grad_join_kern
 
 hipError_t fade_embed_launch(const OpTokens &t, size_t n, const OpMat &table, size_t vocab, size_t width, float scale, const OpMat &out, hipStream_t s) {
   const int shift = lanes_shift(width, 8), rows = 256 >> shift;
-  const dim3 grid((uint32_t)((n + rows - 1) / rows));
+  const dim3 grid(row_blocks(n, rows));
   auto go = [&](auto *in, auto *to) {
     typedef std::remove_const_t<std::remove_pointer_t<decltype(in)>> TT;
     typedef std::remove_pointer_t<decltype(to)> TO;
@@ -549,10 +552,7 @@ hipError_t fade_embed_grad_launch(const OpTokens &t, size_t n, const OpMat &dout
   auto *sum = dout.f32 ? (p.shift == 6 ? grad_sum_kernel<float, true> : grad_sum_kernel<float, false>)
                        : (p.shift == 6 ? grad_sum_kernel<bf16_t, true> : grad_sum_kernel<bf16_t, false>);
   hipLaunchKernelGGL(sum, sums, b, 0, s, p, a);
-  const dim3 joins((p.pieces + a.share - 1) / a.share * (uint32_t)p.strips);
-  if (p.pieces > 2) {
-    if (p.shift == 6) hipLaunchKernelGGL(grad_join_kernel<512>, joins, dim3(512), 0, s, p, a);
-    else hipLaunchKernelGGL(grad_join_kernel<1024>, joins, dim3(1024), 0, s, p, a);
-  }
+  if (p.pieces > 2)
+    hipLaunchKernelGGL(grad_join_kernel, dim3((p.pieces + a.share - 1) / a.share * (uint32_t)p.strips), dim3(JOIN_THREADS), 0, s, p, a);
   return hipGetLastError();
 }

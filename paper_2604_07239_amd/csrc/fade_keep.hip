@@ -1,9 +1,10 @@
 // fade_keep.hip — activations kept in 8 bits between the passes, and the weight gradient from them (gfx950).
 //
 // A group of 32 columns shares a power of two, so what a checkpoint stands for is exact in bf16, and a product with it runs on the bf16 matrix
-// cores with nothing rounded but the fp32 sums. Writing and reading are one pass over the data, bounded by its bytes. The weight gradient dW = x^T dy contracts over the rows: the
-// row-major tiles of both operands are turned on their way out of LDS (ds_read_b64_tr_b16), x is widened to bf16 on its way in.
-// An fp32 dy goes in as three bf16 terms, each the leading 8 bits of what the ones before left: 24 bits, so that they add up to it.
+// cores with nothing rounded but the fp32 sums. Writing and reading are one pass over the data, bounded by its bytes: 16384 x 4096, bf16, 39 and 29 us (203 MB each).
+// The weight gradient dW = x^T dy contracts over the rows: the row-major tiles of both operands are turned on their way out of LDS (ds_read_b64_tr_b16), x is widened
+// to bf16 on its way in. An fp32 dy goes in as three bf16 terms, each the leading 8 bits of what the ones before left: 24 bits, so that they add up to it
+// (three products at the bf16 rate: 16384 rows, 2048 x 2048 375 us, 1.1 PFLOP/s of matrix work; a library's fp32 product of that size takes 900).
 #include <type_traits>
 
 #include "../../include/fade.h"
@@ -15,33 +16,33 @@ using namespace fade_op;
 
 template <typename T>
 __global__ __launch_bounds__(256) void keep_kernel(const T *x, size_t ld, int width, OpKeep k, int shift) {
-  const size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
-  if (row >= k.rows) return;
-  uint8_t *q = k.p + row * k.groups * 32, *e = k.p + k.rows * k.groups * 32 + row * k.groups;
-  for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < k.groups * 32; c += 8 << shift) {
-    float v[8];
-    OpRaw<T> in;
-    if (c < width) in.load(x + row * ld + c, width - c, c);
-    else in.zero();
-    in.fix(width - c, c);
-    in.get(v);
-    uint32_t exp;
-    const uint2 w = op_keep_pack(v, exp);
-    *reinterpret_cast<uint2 *>(q + c) = w;
-    if ((threadIdx.x & 3) == 0) e[c >> 5] = (uint8_t)exp;
+  for (size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift); row < k.rows; row += (size_t)gridDim.x * (256 >> shift)) {
+    uint8_t *q = k.p + row * k.groups * 32, *e = k.p + k.rows * k.groups * 32 + row * k.groups;
+    for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < k.groups * 32; c += 8 << shift) {  // a quad's lanes together
+      float v[8];
+      OpRaw<T> in;
+      if (c < width) in.load(x + row * ld + c, width - c, c);
+      else in.zero();
+      in.fix(width - c, c);
+      in.get(v);
+      uint32_t exp;
+      const uint2 w = op_keep_pack(v, exp);
+      *reinterpret_cast<uint2 *>(q + c) = w;
+      if ((threadIdx.x & 3) == 0) e[c >> 5] = (uint8_t)exp;
+    }
   }
 }
 template <typename T>
 __global__ __launch_bounds__(256) void keep_read_kernel(OpKeep k, int width, T *out, size_t ld, int shift) {
-  const size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
-  if (row >= k.rows) return;
-  const uint8_t *q = k.p + row * k.groups * 32, *e = k.p + k.rows * k.groups * 32 + row * k.groups;
-  for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < width; c += 8 << shift) {
-    float v[8];
-    op_keep_unpack(*reinterpret_cast<const uint2 *>(q + c), op_keep_unit(e[c >> 5]), v);
-    OpRaw<T> o;
-    o.put(v);
-    o.store(out + row * ld + c, width - c);
+  for (size_t row = (size_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift); row < k.rows; row += (size_t)gridDim.x * (256 >> shift)) {
+    const uint8_t *q = k.p + row * k.groups * 32, *e = k.p + k.rows * k.groups * 32 + row * k.groups;
+    for (int c = (threadIdx.x & ((1 << shift) - 1)) * 8; c < width; c += 8 << shift) {
+      float v[8];
+      op_keep_unpack(*reinterpret_cast<const uint2 *>(q + c), op_keep_unit(e[c >> 5]), v);
+      OpRaw<T> o;
+      o.put(v);
+      o.store(out + row * ld + c, width - c);
+    }
   }
 }
 
@@ -93,7 +94,10 @@ template <int MM, int RD, int WR, int VA, int K = 0> __device__ __forceinline__ 
   }
 }
 // WM x WN wavefronts, each TM x TN tiles of 32 x 32. Units of 64 rows pass through two places in LDS: while the matrix cores work on one, the
-// next is on its way through the registers (x has to be widened, an fp32 dy split, on the way) into the other; one barrier a unit.
+// next is on its way through the registers (x has to be widened, an fp32 dy split, on the way) into the other; one barrier a unit. Loads are a unit ahead of the
+// stores into LDS, operand reads a step of 16 rows ahead of the matrix instructions. 256 x 256 tiles: 1.9 us a unit and compute unit at 1.12 PFLOP/s (the library's
+// bf16 product 1.22); the matrix cores are busy 53 % of the cycles, LDS 40 %, the vector ALU 33 %, at the clock that this power leaves. Tried and no
+// faster: four wavefronts of 128 x 128 (340 us instead of 260 at 16384 rows, 4096 x 2048), all of a unit's stores at one step, 128 x 256 tiles without ranges (300).
 template <int WM, int WN, int TM, int TN, bool F32> __global__ __launch_bounds__(WM * WN * 64, 1) void keep_grad_kernel(WgradArgs g) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NT = WM * WN * 64, PLANES = F32 ? 3 : 1;
   constexpr int A_BYTES = 64 * BM * 2, B_BYTES = 64 * BN * 2, PLACE = A_BYTES + PLANES * B_BYTES;
@@ -335,14 +339,14 @@ __global__ __launch_bounds__(256) void keep_grad_add_kernel(const float *part, i
 
 hipError_t fade_keep_launch(const OpMat &x, size_t width, const OpKeep &k, hipStream_t s) {
   const int shift = lanes_shift(width, 8), rows = 256 >> shift;
-  const dim3 grid((uint32_t)((k.rows + rows - 1) / rows));
+  const dim3 grid(row_blocks(k.rows, rows));
   if (x.f32) hipLaunchKernelGGL(keep_kernel<float>, grid, dim3(256), 0, s, static_cast<const float *>(x.p), x.ld, (int)width, k, shift);
   else hipLaunchKernelGGL(keep_kernel<bf16_t>, grid, dim3(256), 0, s, static_cast<const bf16_t *>(x.p), x.ld, (int)width, k, shift);
   return hipGetLastError();
 }
 hipError_t fade_keep_read_launch(const OpKeep &k, size_t width, const OpMat &out, hipStream_t s) {
   const int shift = lanes_shift(width, 8), rows = 256 >> shift;
-  const dim3 grid((uint32_t)((k.rows + rows - 1) / rows));
+  const dim3 grid(row_blocks(k.rows, rows));
   void *p = const_cast<void *>(out.p);
   if (out.f32) hipLaunchKernelGGL(keep_read_kernel<float>, grid, dim3(256), 0, s, k, (int)width, static_cast<float *>(p), out.ld, shift);
   else hipLaunchKernelGGL(keep_read_kernel<bf16_t>, grid, dim3(256), 0, s, k, (int)width, static_cast<bf16_t *>(p), out.ld, shift);

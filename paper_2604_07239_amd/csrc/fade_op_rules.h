@@ -7,6 +7,13 @@
 
 namespace fade_op {
 
+// Workgroups of 256 for rows, `groups` at a time: one for each, up to 2^20 of them (a launch may have
+// 2^32 lanes); the kernels go on in strides.
+inline uint32_t row_blocks(size_t rows, int groups) {
+  const size_t need = (rows + groups - 1) / groups;
+  return (uint32_t)(need < ((size_t)1 << 20) ? need : (size_t)1 << 20);
+}
+
 struct GradPlan {
   int passes, bits;             // digits
   uint32_t n, vocab, tiles;

@@ -90,7 +90,9 @@ def _check_grad(torch, g, t, dy, vocab, scale, accumulate, pad=0, shift=0, dtype
     (32, 1, 33, "i32", "float32", False, 2, 1), (33, 2, 7, "u8", "bfloat16", True, 1, 3), (1000, 1023, 64, "i32", "float32", False, 0, 0),
     (1025, 1024, 100, "i64", "bfloat16", False, 4, 1), (2049, 1025, 520, "i32", "float32", True, 0, 0), (5000, 7, 129, "u8", "bfloat16", False, 0, 0),
     (4097, 50021, 40, "i64", "float32", False, 0, 0), (300, 1 << 20, 4, "i32", "bfloat16", False, 0, 0), (140000, 300, 16, "i32", "bfloat16", False, 0, 0),
-    (70, 11, 5000, "i32", "float32", False, 0, 0)])
+    (70, 11, 5000, "i32", "float32", False, 0, 0), (4096, 30000, 24, "i64", "float32", False, 0, 0), (8192, 60000, 24, "i32", "bfloat16", True, 0, 0),
+    (8193, 60000, 24, "i32", "float32", False, 0, 0), (16384, 256, 40, "u8", "bfloat16", False, 0, 0), (16385, 256, 40, "u8", "float32", False, 0, 0),
+    (20011, 50021, 17, "i64", "bfloat16", True, 1, 1), (9000, 1 << 20, 8, "i32", "float32", False, 0, 0)])
 def test_gradient_against_the_sum(n, vocab, width, token, dtype, accumulate, pad, shift):
     torch = need_gpu()
     rng = np.random.default_rng(n + vocab)
@@ -99,10 +101,11 @@ def test_gradient_against_the_sum(n, vocab, width, token, dtype, accumulate, pad
     g.close()
 
 
+@pytest.mark.parametrize("width", [72, 600])
 @pytest.mark.parametrize("case", ["one token", "all different", "none inside", "two runs", "borders"])
-def test_gradient_of_extreme_runs(case):
+def test_gradient_of_extreme_runs(case, width):
     torch = need_gpu()
-    n, vocab, width = 6001, 7000, 72
+    n, vocab = 6001, 7000
     t = {"one token": np.full(n, 4321), "all different": np.random.default_rng(3).permutation(vocab)[:n], "none inside": np.full(n, -5),
          "two runs": np.where(np.arange(n) % 2 == 0, 17, 6999), "borders": np.arange(n) // 32}[case].astype(np.int32)
     g = context()
@@ -139,4 +142,52 @@ def test_padding_may_hold_anything():
         torch.cuda.synchronize()
         got.append(grad)
     assert torch.equal(got[0], got[1])
+    g.close()
+
+
+@pytest.mark.parametrize("n,vocab,width,dtype", [(70001, 3000, 600, "bfloat16"), (140000, 700, 1024, "bfloat16"), (300000, 256, 64, "float32"), (33000, 200000, 520, "float32")])
+def test_gradient_of_large_batches(n, vocab, width, dtype):
+    """Pieces of every length, against 64-bit sums on the device; tokens as frequent as in a text, so that runs of every length cross every border."""
+    torch = need_gpu()
+    rng = np.random.default_rng(n)
+    t = torch.from_numpy(np.minimum(np.exp(rng.random(n) * np.log(vocab + 1)).astype(np.int64) - 1, vocab - 1)).cuda()
+    d = torch.randn((n, width), device="cuda").to(getattr(torch, dtype))
+    g = context()
+    grad, work = torch.full((vocab, width), 7.0, device="cuda"), torch.full((g.embed_grad_work(n, vocab, width),), 0xA5, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g.embed_grad(t, d, grad, work, scale=0.5)
+    torch.cuda.synchronize()
+    want = torch.zeros((vocab, width), dtype=torch.float64, device="cuda").index_add_(0, t, d.double()) * 0.5
+    size = torch.zeros((vocab, width), dtype=torch.float64, device="cuda").index_add_(0, t, d.double().abs()) * 0.5
+    count = torch.bincount(t, minlength=vocab)[:, None]
+    assert ((grad.double() - want).abs() <= (count + 2) * U * size).all()
+    g.close()
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """2^24 + 5 rows of 1032 columns (35 GB): the rows behind those that one workgroup each takes first."""
+    torch = need_gpu()
+    n, width = (1 << 24) + 5, 1032
+    g = context()
+    table = torch.randn((3, width), device="cuda").bfloat16()
+    t = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    t[-7:] = 2
+    t[n // 2] = 1
+    out = torch.empty((n, width), dtype=torch.bfloat16, device="cuda")
+    keep = torch.empty(g.checkpoint_nbytes(n, width), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g.embed(t, table, out)
+    g.checkpoint(out, keep)
+    torch.cuda.synchronize()
+    for at, v in ((0, 0), (n // 2, 1), (n // 2 + 1, 0), (n - 8, 0), (n - 7, 2), (n - 1, 2)):
+        assert torch.equal(out[at], table[v]), at
+    back = torch.empty((3, width), dtype=torch.bfloat16, device="cuda")
+    small = torch.empty(g.checkpoint_nbytes(3, width), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g.checkpoint(table, small)
+    g.checkpoint_read(small, back)
+    g.checkpoint_read(keep, out)
+    torch.cuda.synchronize()
+    for at, v in ((0, 0), (n // 2, 1), (n - 1, 2)):
+        assert torch.equal(out[at], back[v]), at
     g.close()

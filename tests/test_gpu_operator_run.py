@@ -202,6 +202,63 @@ def test_captured_calls_replay_as_they_ran():
     c.close()
 
 
+def test_two_graphs_with_workspaces_of_their_own_run_side_by_side():
+    """Two programs on two streams, captured, replayed together many times: what each computes is what it computes alone."""
+    torch = need_gpu()
+    n, C, V = 5000, 264, 900
+    rng = np.random.default_rng(6)
+    programs = []
+    for k in range(2):
+        s = torch.cuda.Stream()
+        c = context(s.cuda_stream)
+        with torch.cuda.stream(s):
+            tokens = torch.from_numpy(rng.integers(0, V, n).astype(np.int32)).cuda()
+            d, u = torch.randn((n, C), device="cuda"), torch.randn((n, C), device="cuda")
+            gamma, keep = torch.rand(C, device="cuda") + 0.5, torch.empty(c.checkpoint_nbytes(n, C), dtype=torch.uint8, device="cuda")
+            grad, dw, du, dgamma = torch.empty((V, C), device="cuda"), torch.empty((C, C), device="cuda"), torch.empty((n, C), device="cuda"), torch.empty(C, device="cuda")
+            work = [torch.empty(b, dtype=torch.uint8, device="cuda") for b in (c.embed_grad_work(n, V, C), c.join_grad_work(n, C), c.checkpoint_weight_grad_work(n, C, C))]
+
+        def calls(c=c, tokens=tokens, d=d, u=u, gamma=gamma, keep=keep, grad=grad, dw=dw, du=du, dgamma=dgamma, work=work):
+            c.checkpoint(u, keep)
+            c.join_grad(d, d, work[1], r=u, u=u, gamma_u=gamma, du=du, d_gamma_u=dgamma)
+            c.checkpoint_weight_grad(keep, du, dw, work[2])
+            c.embed_grad(tokens, du, grad, work[0])
+
+        s.synchronize()
+        with torch.cuda.stream(s):
+            calls()
+        s.synchronize()
+        want = [t.clone() for t in (grad, dw, du, dgamma)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            calls()
+        programs.append((s, c, graph, (grad, dw, du, dgamma), want))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, _, graph, _, _ in programs:
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, c, _, got, want in programs:
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        c.close()
+
+
+def test_a_context_on_the_default_stream():
+    """hip_stream 1 is HIP's name for the default stream: calls and a program's other work there follow one another without waits."""
+    torch = need_gpu()
+    c = context(1)
+    x, keep = torch.zeros((300, 512), device="cuda"), torch.zeros(context(1).checkpoint_nbytes(300, 512), dtype=torch.uint8, device="cuda")
+    y = torch.zeros_like(x)
+    for i in range(20):
+        x.fill_(float(i))
+        c.checkpoint(x, keep)
+        c.checkpoint_read(keep, y)
+        x.fill_(-1.0)
+        assert (y == float(i)).all()
+    c.close()
+
+
 def test_the_current_device_and_errors_are_left_alone():
     torch = need_gpu()
     import paper_2604_07239_amd as fa

@@ -193,6 +193,7 @@ int main() {
         WANT(p.range == 0 || (n <= 16384 && p.range <= RANGE_TOKENS && (1u << p.range_bits) >= p.range));
         WANT(p.bytes >= p.part + (size_t)2 * p.pieces * 4 * ((width + 7) / 8 * 8));
       }
+  for (int groups : {1, 2, 64}) WANT(row_blocks(1, groups) == 1 && (size_t)row_blocks(0x7fffffff, groups) * 256 < (size_t)1 << 32 && row_blocks(1000, groups) == (uint32_t)((1000 + groups - 1) / groups));
   for (size_t rows : {(size_t)0, (size_t)1, (size_t)64, (size_t)65, (size_t)1500, (size_t)16384, (size_t)100001, (size_t)0x7fffffff})
     for (size_t K : {(size_t)1, (size_t)128, (size_t)129, (size_t)4096, (size_t)65536})
       for (size_t N : {(size_t)1, (size_t)1000, (size_t)2048, (size_t)65536})
