@@ -240,7 +240,7 @@ enum { FADE_NORM_NONE = 0, FADE_NORM_LAYER = 1, FADE_NORM_RMS = 2 };
 typedef struct {
   uint32_t struct_size;           /* sizeof(fade_join_args) */
   uint32_t norm_u, norm_n;        /* FADE_NORM_* */
-  float eps;                      /* 0 => 1e-5 */
+  float eps;                      /* 0 => 1e-5; else a normal number */
   size_t rows, width;
   uint32_t stream_type;           /* elements of r, h, dh, dr */
   uint32_t branch_type;           /* elements of u, g, n, dn, du, dg: FADE_BF16, or FADE_F32 with an fp32 stream */

@@ -418,6 +418,8 @@ class Fade:
         like = dh if dh is not None else dn
         if like is None:
             self._bad("neither dh nor dn")
+        if like.dim() != 2:
+            self._bad("dh or dn: a matrix is needed")
         rows, width = like.shape
         # the type of each side is that of the first matrix given; a side that nobody gives has any type that goes with the other's
         first_s = r if r is not None else dh if dh is not None else dr

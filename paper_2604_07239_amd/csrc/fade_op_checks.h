@@ -1,6 +1,7 @@
 // fade_op_checks.h — what the entry points of the operators ask of their arguments, as plain C++ (host tests compile it by itself).
 // Each function gives NULL, or what is wrong; nothing here needs a device.
 #pragma once
+#include <cfloat>
 #include <cmath>
 #include <initializer_list>
 #include <stdint.h>
@@ -64,7 +65,7 @@ inline const char *join_model(const fade_join_args *a, bool grad) {
   if (!join_sizes(a->rows, a->width)) return "rows or width out of range";
   if (a->norm_u > FADE_NORM_RMS || a->norm_n > FADE_NORM_RMS) return "unknown norm";
   if (!type(a->stream_type) || !type(a->branch_type) || (a->branch_type == FADE_F32 && a->stream_type == FADE_BF16)) return "types";
-  if (!(a->eps >= 0.0f) || !std::isfinite(a->eps)) return "eps";
+  if (!(a->eps == 0.0f || a->eps >= FLT_MIN) || !std::isfinite(a->eps)) return "eps";  // 1 / sqrt takes a subnormal number for zero
   if (a->lam_count != 0 && a->lam_count != 1 && a->lam_count != a->width) return "lam has neither one value nor one per column";
   if ((a->lam_count != 0) != (a->lam != nullptr)) return "lam and lam_count";
   if (a->norm_u == FADE_NORM_NONE && (a->gamma_u || a->beta_u)) return "parameters of a norm of u that is none";

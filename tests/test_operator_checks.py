@@ -258,3 +258,42 @@ def test_the_binding_refuses_tensors_that_are_not_on_the_device(call):
     with pytest.raises(fa.FadeError) as e:
         getattr(_Ctx(), call)(*args, **({"r": x, "u": x} if call.startswith("join") else {}))
     assert e.value.code == -1
+
+
+EPS = """
+#include <stdio.h>
+#include <string.h>
+#include "fade_op_checks.h"
+int main() {
+  alignas(64) static char mem[64];
+  fade_join_args a;
+  memset(&a, 0, sizeof a);
+  a.struct_size = sizeof a;
+  a.rows = 1; a.width = 8; a.r = a.u = mem; a.h = mem + 32; a.r_ld = a.u_ld = a.h_ld = 8;
+  for (const float eps : {0.0f, 1e-5f, FLT_MIN}) {
+    a.eps = eps;
+    if (const char *why = fade_op::join(&a)) return printf("%g refused: %s\\n", eps, why), 1;
+  }
+  for (const float eps : {FLT_MIN / 2, 1e-45f}) {
+    a.eps = eps;
+    if (!fade_op::join(&a)) return printf("%g not refused\\n", eps), 1;
+  }
+  return 0;
+}
+"""
+
+
+def test_an_eps_that_the_reciprocal_root_takes_for_zero_is_refused(tmp_path):
+    """1 / sqrt of a subnormal number is infinite on the device: a row of equal values would become NaN instead of zeros."""
+    _run(EPS, tmp_path)
+
+
+@pytest.mark.parametrize("shape", [(4,), (2, 3, 8)])
+def test_gradients_that_are_no_matrix_are_refused(shape):
+    torch = pytest.importorskip("torch")
+    import paper_2604_07239_amd as fa
+    ctx = object.__new__(fa.Fade)
+    ctx.h, ctx.device = None, 0
+    for dh, dn in ((torch.zeros(shape), None), (None, torch.zeros(shape))):
+        with pytest.raises(fa.FadeError):
+            ctx.join_grad(dh, dn, None)
