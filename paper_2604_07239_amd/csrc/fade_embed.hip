@@ -6,6 +6,8 @@
 // (stable, hence ascending in every token's run) and cut into pieces of equal length, each summed in order by one group of lanes. The sort moves a
 // few words a token, the sums read dy once and write G once. 32768 tokens of 65536, width 2048, bf16: sort 25 us, sums 130 to 145 (671 MB at 4.6 to 5.2 TB/s: the
 // memory bounds them), long runs 9. 262144 bytes, width 64, fp32: sort 16, sums 14 (67 MB), long runs 13: there launches and dependent loads are most of it.
+// Tried and slower: no sort, but a table of the vocabulary in LDS for each wavefront, which adds its rows to it in order (96 us instead of 46: LDS takes 150 ns for 64
+// float additions, and tables of 64 KB leave two wavefronts a compute unit to wait for them).
 #include "../../include/fade.h"
 #include "fade_op_rules.h"
 #include "fade_ops.h"
