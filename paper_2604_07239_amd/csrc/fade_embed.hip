@@ -5,8 +5,8 @@
 // differ from run to run; a decoder that repeats an encoder's training would leave it. So the positions are sorted by token first
 // (stable, hence ascending in every token's run) and cut into pieces of equal length, each summed in order by one group of lanes. The sort moves a
 // few words a token, the sums read dy once and write G once. 32768 tokens of 65536, width 2048, bf16: sort 25 us, sums 130 to 145 (671 MB at 4.6 to 5.2 TB/s: the
-// memory bounds them), long runs 9. 262144 bytes, width 64, fp32: sort 16, sums 14 (67 MB), long runs 13: there launches and dependent loads are most of it.
-// Tried and slower: no sort, but a table of the vocabulary in LDS for each wavefront, which adds its rows to it in order (96 us instead of 46: LDS takes 150 ns for 64
+// memory bounds them), long runs 9. 262144 bytes, width 64, fp32: sort 16, sums 14 (67 MB), long runs 11: there launches and dependent loads are most of it.
+// Tried and slower: no sort, but a table of the vocabulary in LDS for each wavefront, which adds its rows to it in order (96 us instead of 43: LDS takes 150 ns for 64
 // float additions, and tables of 64 KB leave two wavefronts a compute unit to wait for them).
 #include "../../include/fade.h"
 #include "fade_op_rules.h"
@@ -425,9 +425,10 @@ template <typename T, bool FULL> __global__ __launch_bounds__(256) void grad_sum
 }
 // The runs that reach past the next piece: the workgroup of the pieces they start in adds their parts, its groups of lanes in equal ranges of the pieces
 // in between. A few pieces per workgroup; hardly any has such a run.
-constexpr int JOIN_THREADS = 512;  // 262144 bytes: 13 us; 1024 15, 256 19
+constexpr int JOIN_THREADS = 512;  // 262144 bytes: 11 us; of four parts on their way at a time, 13 with 512, 15 with 1024, 19 with 256 (16 parts: 13)
 __global__ __launch_bounds__(JOIN_THREADS) void grad_join_kernel(GradPlan p, SumArgs a) {
   __shared__ __align__(16) float sums[JOIN_THREADS][8];
+  constexpr uint32_t AHEAD = 8;
   const uint32_t block = blockIdx.x / p.strips, P = p.piece;
   const int strip = (int)(blockIdx.x - block * p.strips), group = threadIdx.x >> p.shift, groups = JOIN_THREADS >> p.shift;
   const int lane = threadIdx.x & ((1 << p.shift) - 1), c = (strip << (p.shift + 3)) + lane * 8;
@@ -454,17 +455,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void grad_join_kernel(GradPlan p, Sum
         o.load(a.part + ((size_t)piece * 2 + 1) * a.part_ld + c, 8);
         o.get(acc);
       }
-      for (uint32_t i = from; i < to; i += 4) {
-        OpRaw<float> o[4];
+      // several parts on their way together; past the last one it comes again, for nothing
+      const float *src = a.part + c;
+      const size_t step = (size_t)2 * a.part_ld;
+      for (uint32_t i = from; i < to; i += AHEAD) {
+        OpRaw<float> o[AHEAD];
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) o[j].load(a.part + (size_t)(i + j < to ? i + j : to - 1) * 2 * a.part_ld + c, 8);
+        for (uint32_t j = 0; j < AHEAD; ++j) o[j].load(src + (i + j < to ? i + j : to - 1) * step, 8);
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-          if (i + j >= to) break;
+        for (uint32_t j = 0; j < AHEAD; ++j) {
           float x[8];
           o[j].get(x);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) acc[k] += x[k];
+          for (int k = 0; k < 8; ++k) acc[k] += i + j < to ? x[k] : 0.0f;
         }
       }
     }
