@@ -1,4 +1,4 @@
-"""The sizes that the GPU tests of several turns run are what they are meant to be, and the bars of the join's gradients let no
+"""The sizes that the GPU tests of several turns and of large tiles run are what they are meant to be, and the bars of the join's gradients let no
 wrong one through. No device is needed."""
 import os
 import subprocess
@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from join_reference import MODELS, STEPS, TYPES, backward, forward, model, rows_wrong, sums_wrong
-from operator_shapes import JOIN_TURNS
+from operator_shapes import JOIN_TURNS, WEIGHT_GRADS
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PLANS = """
@@ -18,10 +18,13 @@ PLANS = """
 using namespace fade_op;
 int main(int argc, char **argv) {
   for (int i = 1; i + 3 < argc; i += 4) {
-    const size_t rows = atoll(argv[i]), a = atoll(argv[i + 1]);
+    const size_t rows = atoll(argv[i]), a = atoll(argv[i + 1]), b = atoll(argv[i + 2]);
     if (argv[i + 3][0] == 'j') {
       const JoinShape s = join_shape(a);
       printf("%d %d %d %d\\n", s.lanes, s.groups, turn_blocks(rows, s.groups, 2048), grad_blocks(rows, a));
+    } else {
+      const WgradPlan p = wgrad_plan(rows, a, b, argv[i + 3][0] == 'f');
+      printf("%d %d %d\\n", p.large, p.ranges, p.per);
     }
   }
 }
@@ -43,6 +46,17 @@ def test_joins_of_several_turns(tmp_path):
         assert rows % (there * groups) and rows % (back * groups)  # the last one of some workgroups only
         seen |= {lanes, (lanes >= 512, C % 8 == 0)}
     assert seen >= {16, 32, 64, 128, 256, 512, 1024, (False, False), (False, True), (True, False), (True, True)}
+
+
+def test_weight_gradients_of_large_tiles(tmp_path):
+    plans = _plans(tmp_path, [(r, K, N, "f" if t == "float32" else "b") for r, K, N, t, *_ in WEIGHT_GRADS])
+    seen = set()
+    for (rows, K, N, t, accumulate, pad, _, large, ranges, add), (l, r, _) in zip(WEIGHT_GRADS, plans):
+        assert (bool(l), r) == (large, ranges) and add == (0 if r == 1 else 4 if K * N >= 1 << 22 else 1)
+        seen |= {(large, t, r > 1), (t, add), (large, accumulate), (add, pad > 0)}
+        assert rows % 64
+    assert seen >= {(True, t, r) for t in ("float32", "bfloat16") for r in (False, True)} | {(t, a) for t in ("float32", "bfloat16") for a in (0, 1, 4)}
+    assert seen >= {(True, True), (True, False), (4, True), (4, False), (1, True), (1, False)}
 
 
 @pytest.mark.parametrize("i", range(len(MODELS)))
