@@ -144,8 +144,8 @@ def _late_type(table, t):
     """torch is the caller's: its types are looked up when the first tensor comes."""
     if not _TYPES:
         import torch
-        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
         _TOKENS.update({torch.uint8: TOKEN_U8, torch.int32: TOKEN_I32, torch.int64: TOKEN_I64})
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})  # last: another thread takes it for both
     return table.get(t.dtype)
 
 
