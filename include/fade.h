@@ -213,7 +213,8 @@ int fade_embed_grad(fade_ctx *ctx, const void *tokens_dev, int token_type, size_
                     size_t work_bytes);
 
 /* Activation checkpoint of x [rows][width]: 8 bits an element, kept between the passes instead of x. In groups of 32 columns (the last one filled up
- * with zeros): e the least exponent >= -126 with max|x| <= 127 * 2^e, q = x * 2^-e rounded to the nearest integer, ties to even.
+ * with zeros): e the least exponent >= -126 with max|x| <= 127 * 2^e, q = x * 2^-e rounded to the nearest integer, ties to even; where no
+ * e <= 121 reaches max|x| (finite values above 127 * 2^121), e is 121 and q at most 127 in magnitude, so that what is read back is finite.
  * Layout: q as signed bytes [rows][32 G], then e + 127 as bytes [rows][G], G = ceil(width / 32), on an address that is a multiple of 16. A group that holds an infinity or
  * NaN has the exponent byte 255 and reads back as NaN. q * 2^e is exact in bf16. width is at most 2^20.
  *   fade_checkpoint_nbytes: 33 G rows (0 for sizes the calls refuse).

@@ -155,11 +155,12 @@ template <> struct OpRaw<float> {
 // 8-bit checkpoints: a group of 32 columns is four lanes of 8 columns each, neighbours inside a quad.
 // ---------------------------------------------------------------------------------------------------
 // Exponent byte e + 127 of a group from the bits of its largest magnitude: with top = m 2^k, 127 = 1.984375 * 2^6, the least e is k - 6, or k - 5
-// where m > 1.984375 (mantissa bits over 0x7e0000); 255: an infinity or NaN is among them.
+// where m > 1.984375 (mantissa bits over 0x7e0000), 121 at most; 255: an infinity or NaN is among them.
+constexpr uint32_t OP_KEEP_EXP_MAX = 121 + 127;
 __device__ __forceinline__ uint32_t op_keep_exp(uint32_t top) {
   const int k = (int)(top >> 23);
   const int e = k - 6 + ((top & 0x7fffffu) > 0x7e0000u ? 1 : 0);
-  return k == 255 ? 255u : (uint32_t)(e < 1 ? 1 : e);
+  return k == 255 ? 255u : e < 1 ? 1u : (uint32_t)e > OP_KEEP_EXP_MAX ? OP_KEEP_EXP_MAX : (uint32_t)e;
 }
 // 2^e of an exponent byte; 255 gives an infinity: 0 * infinity is the NaN such a group reads back as (its bytes are zeros)
 __device__ __forceinline__ float op_keep_unit(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
@@ -185,6 +186,11 @@ __device__ __forceinline__ uint2 op_keep_pack(const float x[8], uint32_t &e) {
   uint32_t q[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, fmaf(x[i], inv, 12582912.0f));
+  if (e == OP_KEEP_EXP_MAX) {  // 127 * 2^121 is the largest value a byte stands for: 64 * 2^122, the nearest above it, is past fp32
+    const float most = 127.0f * 0x1p121f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, fmaf(fminf(fmaxf(x[i], -most), most), inv, 12582912.0f));
+  }
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
