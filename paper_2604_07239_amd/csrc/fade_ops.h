@@ -160,7 +160,7 @@ constexpr uint32_t OP_KEEP_EXP_MAX = 121 + 127;
 __device__ __forceinline__ uint32_t op_keep_exp(uint32_t top) {
   const int k = (int)(top >> 23);
   const int e = k - 6 + ((top & 0x7fffffu) > 0x7e0000u ? 1 : 0);
-  return k == 255 ? 255u : e < 1 ? 1u : (uint32_t)e > OP_KEEP_EXP_MAX ? OP_KEEP_EXP_MAX : (uint32_t)e;
+  return k == 255 ? 255u : (uint32_t)min(max(e, 1), (int)OP_KEEP_EXP_MAX);
 }
 // 2^e of an exponent byte; 255 gives an infinity: 0 * infinity is the NaN such a group reads back as (its bytes are zeros)
 __device__ __forceinline__ float op_keep_unit(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
@@ -171,7 +171,8 @@ __device__ __forceinline__ uint32_t op_quad_max(uint32_t v) {  // over the four 
   return v > o ? v : o;
 }
 // The 8 bytes of this lane's columns and the group's exponent byte. Every lane of the quad takes part; columns that do not exist hold zeros.
-// x 2^-e + 1.5 * 2^23 is rounded to a whole number, ties to even, whose two's complement is in its low bits: one instruction a value.
+// x 2^-e + 1.5 * 2^23 is rounded to a whole number, ties to even, whose two's complement is in its low bits: one instruction a value, and one that keeps it within 127
+// where the exponent is at its end (for all groups: a branch for those alone took registers that cost the join one of four wavefronts: 149 us instead of 139 at 9000 x 4095).
 __device__ __forceinline__ uint2 op_keep_pack(const float x[8], uint32_t &e) {
   // bits of magnitudes are in the magnitudes' order, infinities and NaNs on top
   uint32_t top = 0;
@@ -185,12 +186,7 @@ __device__ __forceinline__ uint2 op_keep_pack(const float x[8], uint32_t &e) {
   const float inv = __builtin_bit_cast(float, (254u - e) << 23);
   uint32_t q[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, fmaf(x[i], inv, 12582912.0f));
-  if (e == OP_KEEP_EXP_MAX) {  // 127 * 2^121 is the largest value a byte stands for: 64 * 2^122, the nearest above it, is past fp32
-    const float most = 127.0f * 0x1p121f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, fmaf(fminf(fmaxf(x[i], -most), most), inv, 12582912.0f));
-  }
+  for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(fmaf(x[i], inv, 12582912.0f), 12582912.0f - 127.0f, 12582912.0f + 127.0f));
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
