@@ -109,6 +109,10 @@ template <int L> struct RowSums {
     rstd = norm == FADE_NORM_NONE ? 1.0f : __builtin_amdgcn_rsqf(fmaf(sq, inv, eps));  // good to an ulp
   }
 };
+// The factor of (x - mean) where a row is normalised: 1 / sigma. Columns that do not exist hold x = 0 there, and where mean / sigma is past fp32 they would put an infinity, and
+// their parameters' zeros a NaN, into the row's sums. Such a row is level, its variance far below the square of mean's last place, so that every x - mean is zero
+// and any factor right: zero. A NaN stays one.
+__device__ __forceinline__ float factor(float rstd, float mean) { return fabsf(mean) * rstd > 1e38f ? 0.0f : rstd; }
 
 // 8 columns of a parameter; `otherwise` where there is none, zeros past the row's end
 __device__ __forceinline__ void param8(const float *p, float otherwise, int c, int left, float x[8]) {
@@ -216,9 +220,10 @@ template <int L, typename TS, typename TB, bool WHOLE, bool KEEP = true> __globa
     if (KEEP && a.keep_u) keep_row(a.keep_u, a.rows, a.width, row, in, x, l.c);
     if (KEEP && a.keep_g) keep_row(a.keep_g, a.rows, a.width, row, in, g, l.c);
     if (a.norm_u != FADE_NORM_NONE) {
+      const float by = factor(rstd_u, mean_u);
       gu.get(p); bu.get(q);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = fmaf((x[k] - mean_u) * rstd_u, p[k], q[k]);
+      for (int k = 0; k < 8; ++k) x[k] = fmaf((x[k] - mean_u) * by, p[k], q[k]);
     }
     lam.get(p);
 #pragma unroll
@@ -237,9 +242,10 @@ template <int L, typename TS, typename TB, bool WHOLE, bool KEEP = true> __globa
     rs.whole(a.norm_u, v[2], v[3], a.eps, mean_u, rstd_u);
     if (!has_n) continue;
     if (norm_n != FADE_NORM_NONE) {
+      const float by = factor(rstd, mean);
       gn.get(p); bn.get(q);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) h[k] = fmaf((h[k] - mean) * rstd, p[k], q[k]);
+      for (int k = 0; k < 8; ++k) h[k] = fmaf((h[k] - mean) * by, p[k], q[k]);
     }
     OpRaw<TB> o;
     o.put(h);
@@ -365,11 +371,12 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
 #pragma unroll
       for (int k = 0; k < 8; ++k) r[k] = sg[k] = t[k] = e[k] = uhat[k] = 0.0f;
     if (a.norm_u != FADE_NORM_NONE) {
+      const float by = factor(rstd_u, mean_u);
       float q[8];
       gu.get(w); bu.get(q);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        uhat[k] = (uhat[k] - mean_u) * rstd_u;
+        uhat[k] = (uhat[k] - mean_u) * by;
         z[k] = fmaf(uhat[k], w[k], q[k]);
       }
     } else {
@@ -404,8 +411,9 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
       rs.exchange(v);
       rs.whole(a.norm_n, v[0], v[1], a.eps, mean, rstd);
       const float along = rs.over_waves(fmaf(v[0] - mean, v[2], v[3])) * rstd * rs.inv, level = a.norm_n == FADE_NORM_LAYER ? rs.over_waves(v[2]) * rs.inv : 0.0f;
+      const float by = factor(rstd, mean);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) h[k] = (h[k] - mean) * rstd;
+      for (int k = 0; k < 8; ++k) h[k] = (h[k] - mean) * by;
       part.template update<PART_GN>([&](float s, int k) { return fmaf(e[k], h[k], s); });
 #pragma unroll
       for (int k = 0; k < 8; ++k) t[k] = fmaf(rstd, fmaf(-h[k], along, fmaf(e[k], w[k], -level)), t[k]);

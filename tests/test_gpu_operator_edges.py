@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from gpu_helpers import need_gpu
+from join_reference import STEPS, backward, forward, rows_wrong, sums_wrong
 from operator_helpers import U, context, f64
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +59,61 @@ def test_the_largest_values_come_back_finite(dtype):
     total = want.sum(0)[:, None] * 2.0 ** -9
     assert ((np.abs(f64(grad) - total) <= bound) | (np.isnan(total) & np.isnan(f64(grad)))).all()
     g.close()
+
+
+def _level(torch, rows, C, at, seed, of):
+    """Operands of which row `at` of u or of r (and so of h) is 2^114 throughout, whose distance from its mean is zero, and the same with zeros there, for a norm that
+    takes the mean away the same operands; eps is so small that 2^114 / sigma is past fp32."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    r, u, g, dh, dn = (torch.randn((rows, C), device="cuda", generator=gen) for _ in range(5))
+    p = {k: 1.0 + 0.1 * torch.randn(C, device="cuda", generator=gen) for k in ("gamma_u", "beta_u", "gamma_n", "beta_n")}
+    p["lam"] = torch.full((1,), 2.0, device="cuda")
+    if of == "u":
+        u[at] = 2.0 ** 114
+        plain = (r, u.clone())
+        plain[1][at] = 0.0
+    else:
+        g = None
+        p = {k: p[k] for k in ("gamma_n", "beta_n", "lam")}
+        r[at], u[at] = 2.0 ** 114, 0.0
+        dn, dh = 1e-7 * dn, 0.1 * dh
+        plain = (r.clone(), u)
+        plain[0][at] = 0.0
+    return r, u, g, p, dh, dn, plain
+
+
+@pytest.mark.parametrize("of", ["u", "r"])
+@pytest.mark.parametrize("rows,C,at", [(64, 31, 5), (64, 40, 5), (16, 777, 5), (2, 8000, 1)])
+def test_a_level_row_far_from_zero(rows, C, at, of):
+    """Its normalised values are zeros; those of columns that do not exist, behind the width up to the lanes of a row, may be nothing else."""
+    torch = need_gpu()
+    eps, c = 1e-12, context()
+    r, u, g, p, dh, dn, plain = _level(torch, rows, C, at, C, of)
+    norm_u = "layer" if of == "u" else "none"
+    h, n = torch.empty_like(r), torch.empty_like(r)
+    keep = [torch.empty(c.checkpoint_nbytes(rows, C), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    c.join(h, n, r=r, u=u, g=g, norm_u=norm_u, norm_n="layer", eps=eps, keep_n=keep[0], **p)
+    c.checkpoint(n, keep[1])
+    torch.cuda.synchronize()
+    p64, g64 = {k: v.double() for k, v in p.items()}, None if g is None else g.double()
+    f = forward(plain[0].double(), plain[1].double(), g64, p64, norm_u, "layer", eps)
+    assert rows_wrong(n.double(), f["n"], f["m_n"], STEPS["n"], False) == 0
+    if of == "u":
+        assert rows_wrong(h.double(), f["h"], f["m_h"], STEPS["h"], False) == 0
+    assert torch.equal(*keep)
+    out = {k: torch.empty_like(r) for k in ("dr", "du") + (("dg",) if of == "u" else ())}
+    out.update({"d_" + k: torch.empty_like(v) for k, v in p.items()})
+    work = torch.empty(c.join_grad_work(rows, C), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    c.join_grad(dh, dn, work, r=r, u=u, g=g, norm_u=norm_u, norm_n="layer", eps=eps, **p, **out)
+    torch.cuda.synchronize()
+    values, params = backward(plain[0].double(), plain[1].double(), g64, p64, norm_u, "layer", dh.double(), dn.double(), eps)
+    if of == "r":  # the only one in which the row's level is
+        t, m = (x / 2.0 for x in values["dr"])
+        params["d_lam"] = (t * r.double(), m * r.double().abs())
+    for k, (want, made) in values.items():
+        assert rows_wrong(out[k].double(), want, made, STEPS[k], False) == 0, k
+    for k, (terms, made) in params.items():
+        assert sums_wrong(out[k].double(), terms, made) is None, k
+    c.close()
