@@ -105,7 +105,7 @@ template <int L> struct RowSums {
   }
   __device__ __forceinline__ void whole(int norm, float m, float q, float eps, float &mean, float &rstd) const {
     mean = W > 1 ? quotient(over_waves(m * theirs), (float)width, inv) : m;
-    const float d = m - mean, sq = over_waves(W > 1 ? fmaf(d * d, theirs, q) : q);
+    const float d = m - mean, sq = over_waves(W > 1 ? fmaf(d * theirs, d, q) : q);  // in this order: d^2 may be past fp32 where a wavefront has no columns
     rstd = norm == FADE_NORM_NONE ? 1.0f : __builtin_amdgcn_rsqf(fmaf(sq, inv, eps));  // good to an ulp
   }
 };

@@ -82,10 +82,7 @@ def _level(torch, rows, C, at, seed, of):
     return r, u, g, p, dh, dn, plain
 
 
-@pytest.mark.parametrize("of", ["u", "r"])
-@pytest.mark.parametrize("rows,C,at", [(64, 31, 5), (64, 40, 5), (16, 777, 5), (2, 8000, 1)])
-def test_a_level_row_far_from_zero(rows, C, at, of):
-    """Its normalised values are zeros; those of columns that do not exist, behind the width up to the lanes of a row, may be nothing else."""
+def _check_level(rows, C, at, of):
     torch = need_gpu()
     eps, c = 1e-12, context()
     r, u, g, p, dh, dn, plain = _level(torch, rows, C, at, C, of)
@@ -117,3 +114,17 @@ def test_a_level_row_far_from_zero(rows, C, at, of):
     for k, (terms, made) in params.items():
         assert sums_wrong(out[k].double(), terms, made) is None, k
     c.close()
+
+
+@pytest.mark.parametrize("of", ["u", "r"])
+@pytest.mark.parametrize("rows,C,at", [(64, 31, 5), (64, 40, 5), (16, 777, 5), (2, 8000, 1)])
+def test_a_level_row_far_from_zero(rows, C, at, of):
+    """Its normalised values are zeros; those of columns that do not exist, behind the width up to the lanes of a row, may be nothing else."""
+    _check_level(rows, C, at, of)
+
+
+@pytest.mark.parametrize("of", ["u", "r"])
+@pytest.mark.parametrize("rows,C,at", [(3, 1500, 1), (2, 3000, 1), (2, 7000, 0)])
+def test_a_level_row_where_wavefronts_of_the_row_have_no_columns(rows, C, at, of):
+    """A wavefront without columns has nothing to add to the row's variance, however far its mean of nothing is from the row's."""
+    _check_level(rows, C, at, of)
