@@ -367,9 +367,11 @@ template <int L, typename TS, typename TB, bool KEPT, bool WHOLE> __global__ __l
     float z[8], sg[8], r[8], t[8], e[8], w[8];
     arrived<WHOLE>(raw_r, l).get(r); arrived<WHOLE>(raw_g, l).get(sg); arrived<WHOLE>(raw_dh, l).get(t); arrived<WHOLE>(raw_dn, l).get(e);
     load(row + gridDim.x * GROUPS);
-    if (!in)  // a row that is not there adds zeros
+    if (!in) {  // a row that is not there adds zeros; its statistics are the last row's, and nothing times them is to be anything else
 #pragma unroll
       for (int k = 0; k < 8; ++k) r[k] = sg[k] = t[k] = e[k] = uhat[k] = 0.0f;
+      mean_u = rstd_u = 0.0f;
+    }
     if (a.norm_u != FADE_NORM_NONE) {
       const float by = factor(rstd_u, mean_u);
       float q[8];

@@ -61,31 +61,32 @@ def test_the_largest_values_come_back_finite(dtype):
     g.close()
 
 
-def _level(torch, rows, C, at, seed, of):
-    """Operands of which row `at` of u or of r (and so of h) is 2^114 throughout, whose distance from its mean is zero, and the same with zeros there, for a norm that
-    takes the mean away the same operands; eps is so small that 2^114 / sigma is past fp32."""
+def _level(torch, rows, C, at, seed, of, level, gamma):
+    """Operands of which row `at` of u or of r (and so of h) is `level` throughout, whose distance from its mean is zero, and the same with zeros there, for a norm that
+    takes the mean away the same operands; eps is so small that level / sigma is near the end of fp32 or past it."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
     r, u, g, dh, dn = (torch.randn((rows, C), device="cuda", generator=gen) for _ in range(5))
     p = {k: 1.0 + 0.1 * torch.randn(C, device="cuda", generator=gen) for k in ("gamma_u", "beta_u", "gamma_n", "beta_n")}
     p["lam"] = torch.full((1,), 2.0, device="cuda")
     if of == "u":
-        u[at] = 2.0 ** 114
+        u[at] = level
+        p["gamma_u"] *= gamma
         plain = (r, u.clone())
         plain[1][at] = 0.0
     else:
         g = None
         p = {k: p[k] for k in ("gamma_n", "beta_n", "lam")}
-        r[at], u[at] = 2.0 ** 114, 0.0
+        r[at], u[at] = level, 0.0
         dn, dh = 1e-7 * dn, 0.1 * dh
         plain = (r.clone(), u)
         plain[0][at] = 0.0
     return r, u, g, p, dh, dn, plain
 
 
-def _check_level(rows, C, at, of):
+def _check_level(rows, C, at, of, level=2.0 ** 114, gamma=1.0):
     torch = need_gpu()
     eps, c = 1e-12, context()
-    r, u, g, p, dh, dn, plain = _level(torch, rows, C, at, C, of)
+    r, u, g, p, dh, dn, plain = _level(torch, rows, C, at, C, of, level, gamma)
     norm_u = "layer" if of == "u" else "none"
     h, n = torch.empty_like(r), torch.empty_like(r)
     keep = [torch.empty(c.checkpoint_nbytes(rows, C), dtype=torch.uint8, device="cuda") for _ in range(2)]
@@ -128,3 +129,11 @@ def test_a_level_row_far_from_zero(rows, C, at, of):
 def test_a_level_row_where_wavefronts_of_the_row_have_no_columns(rows, C, at, of):
     """A wavefront without columns has nothing to add to the row's variance, however far its mean of nothing is from the row's."""
     _check_level(rows, C, at, of)
+
+
+@pytest.mark.parametrize("level,gamma", [(2.0 ** 114, 1.0), (2.0 ** 106, 16.0)])
+@pytest.mark.parametrize("rows,C,at", [(3, 128, 2), (3, 512, 2), (18, 100, 17)])
+def test_a_level_row_at_the_end_of_a_batch(rows, C, at, level, gamma):
+    """The rows that a workgroup has beside the last one, and that do not exist, add nothing to the parameters' gradients: with the last row's statistics their zeros would be
+    2^106 / sigma = 8e37 away from its mean, and gamma past fp32."""
+    _check_level(rows, C, at, "u", level, gamma)
