@@ -587,6 +587,7 @@ size_t fade_join_grad_bytes(size_t rows, size_t width) {
   return 4 * (blocks ? blocks : 1) * PARTS * part_width((int)width);
 }
 hipError_t fade_join_grad_launch(const JoinArgs &a, hipStream_t s) {
+  if (a.rows == 0 && a.accumulate) return hipSuccess;  // not even a zero is added: it would make a positive zero of a negative one
   const JoinShape sh = join_shape(a.width);
   const int blocks = grad_blocks(a.rows, a.width);
   if (blocks) {

@@ -375,6 +375,7 @@ template <int WM, int WN, int TM, int TN, bool F32> static hipError_t wgrad_go(c
 }
 hipError_t fade_keep_grad_launch(const OpKeep &k, size_t in_width, const OpMat &dy, size_t out_width, float *grad, size_t grad_ld, bool accumulate,
                                  void *work, hipStream_t s) {
+  if (k.rows == 0 && accumulate) return hipSuccess;  // not even a zero is added: it would make a positive zero of a negative one
   const WgradPlan p = wgrad_plan(k.rows, in_width, out_width, dy.f32);
   const bool parts = p.ranges > 1;
   const WgradArgs g{k, dy.p, dy.ld, (int)in_width, (int)out_width, p.tiles_m, p.tiles_n, p.ranges, p.units, p.per, parts ? static_cast<float *>(work) : grad,

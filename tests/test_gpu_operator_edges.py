@@ -137,3 +137,18 @@ def test_a_level_row_at_the_end_of_a_batch(rows, C, at, level, gamma):
     """The rows that a workgroup has beside the last one, and that do not exist, add nothing to the parameters' gradients: with the last row's statistics their zeros would be
     2^106 / sigma = 8e37 away from its mean, and gamma past fp32."""
     _check_level(rows, C, at, "u", level, gamma)
+
+
+def test_a_batch_of_no_rows_leaves_sums_alone_to_the_bit():
+    """Added to a negative zero, a sum of nothing would make it a positive one."""
+    torch = need_gpu()
+    c = context()
+    none, gamma = torch.zeros((0, 40), device="cuda"), torch.ones(40, device="cuda")
+    d, grad = torch.full((40,), -0.0, device="cuda"), torch.full((40, 9), -0.0, device="cuda")
+    work = torch.empty(max(c.join_grad_work(0, 40), c.checkpoint_weight_grad_work(0, 40, 9)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    c.join_grad(none, none, work, r=none, u=none, gamma_u=gamma, d_gamma_u=d, accumulate=True)
+    c.checkpoint_weight_grad(torch.zeros(0, dtype=torch.uint8, device="cuda"), none[:, :9], grad, work, accumulate=True)
+    torch.cuda.synchronize()
+    assert bool(torch.signbit(d).all()) and bool(torch.signbit(grad).all())
+    c.close()
