@@ -379,9 +379,11 @@ class Fade:
         wp, wn = self._bytes(work, "work", 0)
         self._chk(self.L.fade_checkpoint_weight_grad(self.h, kp, rows, k, dp, dk, dld, n, gp, gld, int(accumulate), wp, wn))
 
-    def _join_model(self, width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n):
+    def _join_model(self, width, norm_u, norm_n, eps, lam, gamma_u, beta_u, gamma_n, beta_n):
         if norm_u not in NORMS or norm_n not in NORMS:
             self._bad(f"norm: one of {', '.join(NORMS)} is needed")
+        if not abs(eps) <= 3.4028234663852886e38:  # what is past fp32 can't be packed; the rest is the library's to refuse
+            self._bad("eps: a number of fp32 is needed")
         count = 0
         if lam is not None:
             count = lam.numel()
@@ -402,7 +404,7 @@ class Fade:
         up, branch, ul = self._rows(u, "u", rows, width)
         gp, gl = self._same(g, "g", rows, width, branch)
         np_, nl = self._same(n, "n", rows, width, branch)
-        count, params = self._join_model(width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n)
+        count, params = self._join_model(width, norm_u, norm_n, eps, lam, gamma_u, beta_u, gamma_n, beta_n)
         k = self._keep
         a = _JOIN.pack(_JOIN.size, NORMS[norm_u], NORMS[norm_n], eps, rows, width, stream, branch, count, 0, *params, rp, up, gp, rl, ul, gl, hp, np_, hl, nl,
                        k(keep_r, rows, width), k(keep_u, rows, width), k(keep_g, rows, width), k(keep_n, rows, width), *_NO_GRADS)
@@ -432,7 +434,7 @@ class Fade:
         (rp, rl), (dhp, dhl), (drp, drl) = m(r, "r", rows, width, stream), m(dh, "dh", rows, width, stream), m(dr, "dr", rows, width, stream)
         (up, ul), (gp, gl), (dnp, dnl) = m(u, "u", rows, width, branch), m(g, "g", rows, width, branch), m(dn, "dn", rows, width, branch)
         (dup, dul), (dgp, dgl) = m(du, "du", rows, width, branch), m(dg, "dg", rows, width, branch)
-        count, params = self._join_model(width, norm_u, norm_n, lam, gamma_u, beta_u, gamma_n, beta_n)
+        count, params = self._join_model(width, norm_u, norm_n, eps, lam, gamma_u, beta_u, gamma_n, beta_n)
         v, k = self._vector, self._keep
         a = _JOIN.pack(_JOIN.size, NORMS[norm_u], NORMS[norm_n], eps, rows, width, stream, branch, count, int(accumulate), *params, rp, up, gp, rl, ul, gl, 0, 0, 0, 0,
                        k(keep_r, rows, width), k(keep_u, rows, width), k(keep_g, rows, width), 0, dhp, dnp, dhl, dnl, drp, dup, dgp, drl, dul, dgl,
