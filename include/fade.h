@@ -221,7 +221,7 @@ int fade_embed_grad(fade_ctx *ctx, const void *tokens_dev, int token_type, size_
  *   fade_checkpoint: writes keep_dev from x_dev. fade_checkpoint_read: the values it stands for into out_dev.
  *   fade_checkpoint_weight_grad: the gradient of W in y = x W from x's checkpoint: grad[k][j] = sum over rows of x[row][k] * dy[row][j] (accumulate != 0:
  *     added to grad); keep_dev of [rows][in_width], dy_dev [rows][out_width], grad_dev [in_width][out_width] fp32. Products are exact (an
- *     fp32 dy is taken as three bf16 terms that together are dy), sums fp32. Widths are at most 65536,
+ *     fp32 dy is taken as three bf16 terms that together are dy; below 2^-110 in magnitude they leave out less than 2^-133 of it), sums fp32. Widths are at most 65536,
  *     dy_ld at most 2^22. */
 size_t fade_checkpoint_nbytes(size_t rows, size_t width);
 int fade_checkpoint(fade_ctx *ctx, const void *x_dev, int x_type, size_t x_ld, size_t rows, size_t width, void *keep_dev);

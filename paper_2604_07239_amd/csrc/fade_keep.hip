@@ -65,7 +65,8 @@ __device__ __forceinline__ i16x4 wg_turn(const uint8_t *lds) {  // gfx950's tran
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)lds);
 }
 
-// fp32 as the leading 8 bits, the next 8, the last 8: cut, not rounded, so that nothing overflows and the rest is exact
+// fp32 as the leading 8 bits, the next 8, the last 8: cut, not rounded, so that nothing overflows and the rest is exact (of numbers below 2^-110 down to
+// 2^-133, bf16's smallest, which the matrix cores do not flush)
 __device__ __forceinline__ void wg_split(float v, uint32_t &hi, uint32_t &mid, uint32_t &lo) {
   hi = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
   float rest = v - __builtin_bit_cast(float, hi);

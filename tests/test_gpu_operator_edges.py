@@ -152,3 +152,30 @@ def test_a_batch_of_no_rows_leaves_sums_alone_to_the_bit():
     torch.cuda.synchronize()
     assert bool(torch.signbit(d).all()) and bool(torch.signbit(grad).all())
     c.close()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,K,N,low", [(70, 40, 300, 18), (70, 40, 300, -1), (517, 4090, 4090, 18), (517, 4090, 4090, -1)])
+def test_weight_gradient_of_the_smallest_values(rows, K, N, low, dtype):
+    """The matrix cores take subnormal bf16 as it is, and give subnormal fp32. Of an fp32 dy they get three bf16 terms: all of it from 2^-110 on, whose last bit is bf16's smallest number, 2^-133,
+    below that all but less than 2^-133."""
+    torch = need_gpu()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.zeros((rows, K), device="cuda")
+    x[7] = torch.exp2(torch.randint(low, low + 4, (K,), device="cuda", generator=gen).float())
+    e = torch.randint(-149, -100, (rows, N), device="cuda", generator=gen).double()
+    dy = (torch.exp2(e) * (1 + torch.rand((rows, N), device="cuda", generator=gen).double())).float().to(getattr(torch, dtype))
+    c = context()
+    keep = torch.empty(c.checkpoint_nbytes(rows, K), dtype=torch.uint8, device="cuda")
+    grad = torch.zeros((K, N), device="cuda")
+    work = torch.zeros(c.checkpoint_weight_grad_work(rows, K, N), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    c.checkpoint(x, keep)
+    c.checkpoint_weight_grad(keep, dy, grad, work)
+    torch.cuda.synchronize()
+    err = (grad.double() - x[7].double()[:, None] * dy[7].double()[None]).abs() / x[7].double()[:, None]
+    if dtype == "bfloat16":
+        assert bool((err == 0).all())
+    else:
+        assert bool((err[:, dy[7].double() >= 2.0 ** -110] == 0).all()) and bool((err < 2.0 ** -133).all())
+    c.close()
