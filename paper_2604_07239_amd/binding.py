@@ -271,7 +271,9 @@ class Fade:
 
     # -- operators around a program's own model -----------------------------------------------------
     # Tensors are checked here for what the C ABI cannot see: their device, type, shape and strides. Everything is enqueued on
-    # the context's stream; nothing is allocated.
+    # the context's stream; nothing is allocated. On which of torch's streams a tensor was written is not looked at: give make_config the stream of the
+    # program's other work (hip_stream=stream.cuda_stream; 1 for torch's default stream, whose handle of 0 stands for none), or order the two by events. A
+    # context's own stream (hip_stream=None) and torch's default one wait for each other, at some 20 us a change.
     def _bad(self, what):
         raise FadeError(-1, what)
 
@@ -416,7 +418,8 @@ class Fade:
     def join_grad(self, dh, dn, work, *, r=None, u=None, g=None, keep_r=None, keep_u=None, keep_g=None, lam=None, norm_u="layer", norm_n="layer", gamma_u=None,
                   beta_u=None, gamma_n=None, beta_n=None, eps=0.0, dr=None, du=None, dg=None, d_lam=None, d_gamma_u=None, d_beta_u=None, d_gamma_n=None,
                   d_beta_n=None, accumulate=False):
-        """The gradients of join() for those of h and n (either may be None), from its operands or from their checkpoints."""
+        """The gradients of join() for those of h and n (either may be None), from its operands or from their checkpoints. The block had a gate if g or keep_g
+        is given: without them these are the gradients of a block that had none."""
         like = dh if dh is not None else dn
         if like is None:
             self._bad("neither dh nor dn")
