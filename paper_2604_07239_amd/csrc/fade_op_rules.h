@@ -81,9 +81,10 @@ inline GradPlan grad_plan(size_t n, size_t vocab, size_t width) {
 // The weight gradient K x N over `rows` rows: tiles of the result, and equal ranges of the rows (units of 64) whose sums are added up behind it.
 // Of tile sizes and counts of ranges the cheapest by a model of what was measured, in us: 256 x 256 tiles (fp32 dy: 256 x 128) take 1.85 (2.75) a unit with one
 // workgroup per compute unit, 128 x 128 tiles 0.72 (1.6), or 1.45 with two of them; the first loads and the last stores 10 and 4; sums leave at 5.5 MB/us, and
-// the launch that adds several takes 4.5 more. Measured, the rule's choice | others: 16384 rows, 4096 x 2048, bf16 276 (large, 2) | 420 (large, 1), 364 (small, 1);
-// 4096 rows, 1024 x 1024 26.2 (small, 4) | 34 (2), 28.6 (8), 34.5 (large, 8); 512 rows, 512 x 512 9.6 (small, 1) | 9.7 (2), 17.9 (large, 4); fp32, 16384 rows,
-// 2048 x 2048 383 (large, 2) | 416 (small, 1); 1500 rows, 512 x 1000 18.8 (small, 6) | 19.4 (4), 23.7 (large, 8).
+// the launch that adds several takes 4.5 more. Measured in turn, the rule's choice | others: 16384 rows, 4096 x 2048, bf16 256 (large, 2) | 392 (large, 1), 349 (small, 1);
+// 4096 rows, 1024 x 1024 26 (small, 4) | 33 (2), 27 (8), 33 (large, 8); 512 rows, 512 x 512 8.9 (small, 1) | 9.3 (2), 14.7 (large, 4); fp32, 16384 rows,
+// 2048 x 2048 351 (large, 4, as many as the limit below asks for) | 342 (large, 2), 403 (small, 1); 1500 rows, 512 x 1000 19.2 (small, 8) | 18.0 (6), 18.9 (4),
+// 22.6 (large, 8).
 // A sum over thousands of rows in one fp32 accumulator drifts with its length: no range is longer than 16384 rows, 4096 with fp32 dy's three products a
 // row, until there are 1024 ranges.
 struct WgradPlan {

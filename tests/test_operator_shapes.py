@@ -59,6 +59,12 @@ def test_weight_gradients_of_large_tiles(tmp_path):
     assert seen >= {(True, True), (True, False), (4, True), (4, False), (1, True), (1, False)}
 
 
+def test_the_plans_whose_times_the_rules_quote(tmp_path):
+    """Rows, in, out, type of dy: large tiles, ranges. A change of the rule that moves one of these asks for new figures beside it."""
+    quoted = {(16384, 4096, 2048, "b"): (1, 2), (4096, 1024, 1024, "b"): (0, 4), (512, 512, 512, "b"): (0, 1), (16384, 2048, 2048, "f"): (1, 4), (1500, 512, 1000, "f"): (0, 8)}
+    assert [(large, ranges) for large, ranges, _ in _plans(tmp_path, quoted)] == list(quoted.values())
+
+
 @pytest.mark.parametrize("i", range(len(MODELS)))
 @pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("rows,C", [(700, 60), (61, 777), (2500, 24)])
