@@ -3,12 +3,13 @@
 // A row stays in the registers of the L lanes that own it (8 columns per lane), so each pass reads its operands once and writes its
 // results once, whatever norms and gate there are; the bytes bound it: 16384 x 2048, fp32 stream, bf16 branch 89 us forward (470 MB, 5.2 TB/s); bf16 103 us backward
 // (537 MB). The backward pass forms the statistics again instead of reading saved ones, from the operands themselves or from 8-bit checkpoints of them
-// (8192 x 4096: 118 us, 440 MB: there the two exchanges a row are as long as its bytes).
+// (8192 x 4096: 120 us, 440 MB: there the two exchanges a row are as long as its bytes).
 // LayerNorm's variance is the mean of the squares of centred values: the difference of E[x^2] and mean^2 loses what a large mean covers.
 // Parameter gradients are sums over the rows: a workgroup keeps its columns' sums in registers over all its rows and leaves one partial sum per column,
 // which a second kernel adds in order (4 to 5 us). No atomics.
 // With 8 columns a lane, what a row costs once (exchanges, reciprocals) is half of the vector instructions: sums by DPP shifts, one exchange for several of them and v_rsq
-// took the gradient of 16384 x 2048 from 142 to 103 us. Rows of 1024 lanes (4097 to 8192 columns) have 128 registers a lane: 4096 x 8192 115 us forward, 245 backward.
+// took the gradient of 16384 x 2048 from 142 to 103 us. Rows of 1024 lanes (4097 to 8192 columns) have 128 registers a lane, and their gradient
+// spills 44 to 72 of them: 4096 x 8192, bf16 100 us forward (with three checkpoints 127), 286 backward, 245 from checkpoints.
 // Tried and no faster: two rows on their way instead of one (118 | 118), LDS sums on rows of 512 lanes (118 | 203).
 #include <type_traits>
 

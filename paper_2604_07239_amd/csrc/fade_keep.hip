@@ -1,10 +1,10 @@
 // fade_keep.hip — activations kept in 8 bits between the passes, and the weight gradient from them (gfx950).
 //
 // A group of 32 columns shares a power of two, so what a checkpoint stands for is exact in bf16, and a product with it runs on the bf16 matrix
-// cores with nothing rounded but the fp32 sums. Writing and reading are one pass over the data, bounded by its bytes: 16384 x 4096, bf16, 39 and 29 us (203 MB each).
+// cores with nothing rounded but the fp32 sums. Writing and reading are one pass over the data, bounded by its bytes: 16384 x 4096, bf16, 46 and 30 us, 39 and 29 at best (203 MB each).
 // The weight gradient dW = x^T dy contracts over the rows: the row-major tiles of both operands are turned on their way out of LDS (ds_read_b64_tr_b16), x is widened
 // to bf16 on its way in. An fp32 dy goes in as three bf16 terms, each the leading 8 bits of what the ones before left: 24 bits, so that they add up to it
-// (three products at the bf16 rate: 16384 rows, 2048 x 2048 375 us, 1.1 PFLOP/s of matrix work; a library's fp32 product of that size takes 900).
+// (three products at the bf16 rate: 16384 rows, 2048 x 2048 351 us with the sum of four ranges, 1.17 PFLOP/s of matrix work; a library's fp32 product of that size takes 900).
 #include <type_traits>
 
 #include "../../include/fade.h"
